@@ -284,6 +284,112 @@ ada_status ada_attention_reps(ada_ctx* ctx, const void* Q, const void* K, const 
                               const int32_t* rep_cnt, const int32_t* nearest_idx, float* out,
                               int64_t ldo, uint32_t flags, void* stream);
 
+/*
+ * Paged key / value cache: what a model goes on from after the prompt.  The prompt's keys and values (all of them, or
+ * those of its representatives) are appended to it, and new tokens attend to it.
+ *
+ * A page holds `page_size` slots of every key head.  Slot t of sequence b lies in page table[b * table_ld + t /
+ * page_size], at slot t % page_size.  Pages are head-major: element e of head j and slot s of page p is
+ *     k[p * page_stride + (j * page_size + s) * d_h + e]                 (v alike)
+ * so K and V may be planes of one tensor.  kmin, kmax (both or neither): element e of page p and head j at
+ * (p * h_kv + j) * d_h + e, the elementwise minimum and maximum of the page's keys, which ada_cache_append keeps and
+ * ada_select_blocks reads.  The struct is read during the call; all pointers in it are DEVICE pointers to buffers
+ * that the caller owns.
+ *   - ADA_BF16 only (any context of the device serves, whatever its maxima and its storage type): dt == ADA_F32 is
+ *     ADA_ERR_UNSUPPORTED, as for ada_attention_reps.
+ *   - page_size 16, 32, 64 or 128; d_h a multiple of 16, at most 128; page_stride a multiple of 8, at least
+ *     h_kv * page_size * d_h; K, V, kmin, kmax 16-byte aligned; h_kv <= 4096: else ADA_ERR_UNSUPPORTED.
+ *   - max_pages: entries of a sequence's table row (max_pages * page_size < 2^30).
+ *
+ * The new tokens of all sequences stand one after the other (ragged): sequence b has rows off[b] .. off[b+1] - 1 of
+ * every per-token array, off[0] = 0 <= off[1] <= .. <= off[B] <= N (device, B + 1 entries; a sequence may have none).
+ * Rows from off[B] on are padding: nothing of them is read or written.  len[b] (device) counts the sequence's tokens in
+ * the cache.  Both are read on the device: nothing returns to the host between calls.
+ * Rows of queries hold the heads of a token side by side (head i at i * d_h), rows `ld` elements apart, ld a
+ * multiple of 8, 16-byte aligned: columns of a wider projection will do.  Head i reads key head i / (h / h_kv); h is a
+ * multiple of h_kv, at most 128 times it.
+ *
+ * Device-detected faults (ada_device_status): offsets out of order, a page outside [0, n_pages) where one is
+ * needed, a list that does not ascend (ADA_ERR_BAD_INDEX_SET, also for lengths or counts out of range); NaN or
+ * Inf in what is appended (ADA_ERR_NONFINITE).  What a faulty row gives is meaningless, but in bounds.  Table entries
+ * behind a sequence's length are never looked at, and what is in slots behind it (NaN included) has no influence.
+ */
+typedef struct {
+    void *k, *v;
+    void *kmin, *kmax;
+    const int32_t* table;
+    int64_t table_ld, max_pages, n_pages, page_stride, page_size, h_kv, d_h;
+} ada_kv_cache;
+
+/*
+ * Appends new tokens: row i of sequence b (i from 0) goes to slot len[b] + i.
+ *   K, V     rows of h_kv heads; K is normed (k_norm) and rotated (inv_freq) on the way, V is copied
+ *   Q, q_out optional: rows of h heads, normed (q_norm) and rotated, written to q_out (which may be Q itself)
+ *   q_norm, k_norm  optional, d_h bf16 weights: x_e w_e / sqrt(mean_e x_e^2 + eps) over each head
+ *   inv_freq optional, DEVICE double[rot / 2]: the first `rot` elements of a head (a multiple of 16) are rotated in
+ *            pairs i by the angle position * inv_freq[i], formed in 64 bits: (a, b) -> (a cos - b sin, b cos + a sin).
+ *            The pairs are elements i and i + rot / 2, with ADA_ROPE_PAIRS elements 2 i and 2 i + 1
+ *   pos0     optional, DEVICE int32[B]: position of a sequence's first new token (NULL: len[b]); the tokens after it
+ *            have the positions after it.  A cache that holds only representatives needs it: there a token's
+ *            slot is not its position
+ *   rep_idx, rep_cnt  optional, both or neither: only the rep_cnt[b] tokens rep_idx[off[b]] .. go to the cache, as
+ *            an ascending list of indices within the sequence's new tokens (for sequences of one length T that is the
+ *            layout of ada_select_full and ada_cascade_step).  Each keeps the position that it has in the
+ *            sequence; Q is not affected
+ *   len_out  optional, DEVICE int32[B], not `len` itself: the sequences' new lengths
+ * Arithmetic in fp32, one rounding to bf16.  kmin and kmax of every page written are formed anew from the page's keys
+ * below the new length.  Tokens that the table has no room for are dropped (ADA_ERR_BAD_INDEX_SET).  No page that the
+ * call writes to may belong to two sequences.
+ */
+#define ADA_ROPE_PAIRS 1u
+ada_status ada_cache_append(ada_ctx* ctx, const ada_kv_cache* cache, int64_t B, const int32_t* off, const int32_t* len,
+                            int32_t* len_out, int64_t N, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                            ada_dtype dt, const void* Q, int64_t h, int64_t ldq, void* q_out, int64_t ldqo,
+                            const void* q_norm, const void* k_norm, double eps, const double* inv_freq, int64_t rot,
+                            const int32_t* pos0, const int32_t* rep_idx, const int32_t* rep_cnt, uint32_t flags,
+                            void* stream);
+
+/*
+ * Attention of new tokens over their sequence's cache: out = softmax(scale Q K^T) V per head, one token or a chunk of
+ * them per sequence, also mixed.  len[b] counts the new tokens too (append first).
+ *   max_new  no sequence has more new tokens than this (a sequence that does is ADA_ERR_BAD_INDEX_SET, and its rows from
+ *            max_new on are not written); chooses the kernel, so that it should be tight
+ *   flags    ADA_ATTN_CAUSAL: the sequence's new tokens are its last ones, and each sees the slots up to its own;
+ *            0: each sees all len[b] slots
+ *   scale    of the scores; 0: 1 / sqrt(d_h).  Not negative
+ *   out      bf16, rows of h heads.  A token that sees no slot gets zeros
+ * Scores, softmax statistics and sums in fp32; the probabilities are rounded to bf16 for the second product.
+ * The first call on a context allocates its workspace (40 MB): make it before capturing into a CUDA graph.
+ */
+ada_status ada_attention_cached(ada_ctx* ctx, const ada_kv_cache* cache, int64_t B, const int32_t* off,
+                                const int32_t* len, int64_t N, int64_t max_new, const void* Q, int64_t h, int64_t ldq,
+                                ada_dtype dt, double scale, void* out, int64_t ldo, uint32_t flags, void* stream);
+
+/*
+ * The pages that can matter most to a token: for every new token and key head the k pages p with the largest
+ *     s(p) = sum over the heads g of the key head and e of max(q_ge kmax_pe, q_ge kmin_pe),
+ * which no sum over g of q_g . key of the page exceeds.  The first n_first and the last n_last of the pages that the
+ * token sees are always among them (n_first + n_last <= k); a token that sees at most k pages gets all of them.
+ *   blk_idx  int32 [N][h_kv][k]: places in the sequence's table row, ascending, -1 behind the count
+ *   blk_cnt  int32 [N][h_kv]
+ *   flags    ADA_ATTN_CAUSAL as in ada_attention_cached
+ * The choice is that of scores in 64 bits; equal scores: the lower page; a score that is NaN comes last.  At most 16384
+ * pages per sequence (max_pages, k): else ADA_ERR_UNSUPPORTED.
+ */
+ada_status ada_select_blocks(ada_ctx* ctx, const ada_kv_cache* cache, int64_t B, const int32_t* off, const int32_t* len,
+                             int64_t N, const void* Q, int64_t h, int64_t ldq, ada_dtype dt, int64_t k, int64_t n_first,
+                             int64_t n_last, int32_t* blk_idx, int32_t* blk_cnt, uint32_t flags, void* stream);
+
+/*
+ * ada_attention_cached over listed pages only: token i and key head j see the slots of the pages blk_idx[i][j][0 ..
+ * blk_cnt[i][j] - 1] (an ascending list, as ada_select_blocks leaves it), as far as the token sees them at all.
+ * A token whose list has no such slot gets zeros.  k <= 16384.
+ */
+ada_status ada_attention_blocks(ada_ctx* ctx, const ada_kv_cache* cache, int64_t B, const int32_t* off,
+                                const int32_t* len, int64_t N, const void* Q, int64_t h, int64_t ldq, ada_dtype dt,
+                                const int32_t* blk_idx, const int32_t* blk_cnt, int64_t k, double scale, void* out,
+                                int64_t ldo, uint32_t flags, void* stream);
+
 /* Same operations with HOST buffers: inputs are copied to the device (staging
  * buffers owned by the context, allocated on first use), the device-pointer
  * call above runs, results are copied back, all in the order of `stream` (inputs

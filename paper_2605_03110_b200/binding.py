@@ -21,6 +21,7 @@ ADA_OK = 0
 ADA_F32, ADA_BF16 = 0, 1
 ADA_CROSS_CAUSAL = 1
 ADA_ATTN_CAUSAL = 1
+ADA_ROPE_PAIRS = 1
 ADA_ENGINE_AUTO, ADA_ENGINE_FFMA, ADA_ENGINE_TCGEN05, ADA_ENGINE_TCGEN05_PAIR = 0, 1, 2, 3
 
 SYMBOLS = [
@@ -31,6 +32,7 @@ SYMBOLS = [
     "ada_selftest_launches_alone", "ada_nearest_rep",
     "ada_select_full_heads", "ada_cascade_step_heads", "ada_set_dependent_launch",
     "ada_cascade_step_adaptive", "ada_attention_reps", "ada_set_row_compaction",
+    "ada_cache_append", "ada_attention_cached", "ada_select_blocks", "ada_attention_blocks",
 ]
 ADA_NOALLOC_MAX_T = 16384
 
@@ -42,6 +44,12 @@ class TauPolicy(C.Structure):
     """ada_tau_policy: tau' = clip(tau + gain * (target_turnover - rho), tau_min, tau_max)."""
     _fields_ = [("target_turnover", C.c_double), ("gain", C.c_double), ("tau_min", C.c_double),
                 ("tau_max", C.c_double)]
+
+
+class _KVCacheStruct(C.Structure):
+    """ada_kv_cache"""
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "kmin", "kmax", "table")] + \
+        [(n, C.c_int64) for n in ("table_ld", "max_pages", "n_pages", "page_stride", "page_size", "h_kv", "d_h")]
 
 
 class AdaError(RuntimeError):
@@ -81,6 +89,15 @@ def lib() -> C.CDLL:
         L.ada_nearest_rep.argtypes = [vp, vp, i64, i64, i64, i64, C.c_int, i32p, i32p, i32p, fp, vp]
         L.ada_attention_reps.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, C.c_int, i32p, i32p, i32p, fp,
                                          i64, C.c_uint32, vp]
+        kv = C.POINTER(_KVCacheStruct)
+        L.ada_cache_append.argtypes = [vp, kv, i64, i32p, i32p, i32p, i64, vp, i64, vp, i64, C.c_int, vp, i64, i64, vp,
+                                       i64, vp, vp, C.c_double, vp, i64, i32p, i32p, i32p, C.c_uint32, vp]
+        L.ada_attention_cached.argtypes = [vp, kv, i64, i32p, i32p, i64, i64, vp, i64, i64, C.c_int, C.c_double, vp, i64,
+                                           C.c_uint32, vp]
+        L.ada_select_blocks.argtypes = [vp, kv, i64, i32p, i32p, i64, vp, i64, i64, C.c_int, i64, i64, i64, i32p, i32p,
+                                        C.c_uint32, vp]
+        L.ada_attention_blocks.argtypes = [vp, kv, i64, i32p, i32p, i64, vp, i64, i64, C.c_int, i32p, i32p, i64,
+                                           C.c_double, vp, i64, C.c_uint32, vp]
         L.ada_select_full_host.argtypes = [vp, vp, i64, i64, i64, C.c_int, C.c_double, i32p, i32p, fp, vp]
         L.ada_cascade_step_host.argtypes = [vp, vp, i64, i64, i64, C.c_int, C.c_double,
                                             i32p, i32p, i32p, i32p, i32p, i32p, i32p, i32p, fp, fp,
@@ -131,6 +148,15 @@ def _stream(stream) -> int:
         if _raw_stream is None:
             return torch.cuda.current_stream().cuda_stream
         return _raw_stream(_current_device())
+    return stream.cuda_stream
+
+
+def _stream_of(ctx, stream) -> int:
+    """The current stream of the context's device, whichever device is the current one."""
+    if stream is None:
+        if _raw_stream is None:
+            return torch.cuda.current_stream(ctx.device).cuda_stream
+        return _raw_stream(ctx.device)
     return stream.cuda_stream
 
 
@@ -380,6 +406,182 @@ def ada_attention_reps(ctx: Context, Q: torch.Tensor, K: torch.Tensor, V: torch.
                               out.stride(0), flags, _stream(stream))
     if st:
         _raise(st, "ada_attention_reps")
+    return out
+
+
+class KVCache:
+    """Paged key / value cache: K and V (n_pages, h_kv, page_size, d_h) bf16, planes of one tensor or tensors of their
+    own with the same page stride; table (B, pages of a sequence) int32; kmin, kmax (n_pages, h_kv, d_h) bf16, the
+    bounds of every page's keys (both or neither; ada_select_blocks needs them).  The tensors are the caller's."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, kmin: Optional[torch.Tensor] = None,
+                 kmax: Optional[torch.Tensor] = None):
+        if K.dim() != 4 or V.shape != K.shape or V.stride(0) != K.stride(0) and K.shape[0] > 1:
+            raise ValueError("K and V must be (n_pages, h_kv, page_size, d_h) with the same page stride")
+        n, h_kv, ps, d = K.shape
+        for t in (K, V):
+            if t.stride()[1:] != (ps * d, d, 1):
+                raise ValueError("a page of K or V must be dense: (h_kv, page_size, d_h)")
+        if table.dim() != 2 or table.stride(1) != 1:
+            raise ValueError("table must be (B, pages) with unit inner stride")
+        _int32(table, "table")
+        if (kmin is None) != (kmax is None):
+            raise ValueError("kmin and kmax belong together")
+        for t in (kmin, kmax):
+            if t is not None and (t.shape != (n, h_kv, d) or not t.is_contiguous()):
+                raise ValueError("kmin and kmax must be dense (n_pages, h_kv, d_h)")
+        dtype = dtype_of(K)
+        if any(t is not None and t.dtype != K.dtype for t in (V, kmin, kmax)):
+            raise TypeError("K, V, kmin and kmax must have one type")
+        if any(t is not None and t.device != K.device for t in (V, table, kmin, kmax)):
+            raise ValueError("the cache's tensors must be on one device")
+        self.K, self.V, self.table, self.kmin, self.kmax = K, V, table, kmin, kmax
+        self.dtype, self.h_kv, self.d_h, self.page_size, self.B = dtype, h_kv, d, ps, table.shape[0]
+        self._c = _KVCacheStruct(K.data_ptr(), V.data_ptr(), _ptr(kmin), _ptr(kmax), table.data_ptr(),
+                                 max(table.stride(0), table.shape[1]), table.shape[1], n,
+                                 K.stride(0) if n > 1 else h_kv * ps * d, ps, h_kv, d)
+        self.addr = C.addressof(self._c)
+
+
+def _int32(t: torch.Tensor, name: str, n: Optional[int] = None) -> None:
+    if t.dtype != torch.int32:
+        raise TypeError(f"{name} must be int32")
+    if n is not None and (t.numel() < n or not t.is_contiguous()):
+        raise ValueError(f"{name} must be dense with at least {n} entries")
+
+
+def _ragged(cache: KVCache, off: torch.Tensor, length: torch.Tensor) -> int:
+    """Sequences of a call: off has one entry more than there are, the table and the lengths one for each."""
+    B = off.numel() - 1
+    if B < 1 or B > cache.B:
+        raise ValueError("off must have B + 1 entries, the cache's table at least B rows")
+    _int32(off, "off", B + 1)
+    _int32(length, "the lengths", B)
+    return B
+
+
+def _rows_of(X: torch.Tensor, name: str, cache: KVCache, N: Optional[int] = None):
+    """(N, heads, row stride) of per-token rows (N, heads, d_h), heads side by side."""
+    if X.dim() != 3 or X.shape[2] != cache.d_h or N is not None and X.shape[0] != N:
+        raise ValueError(f"{name} must be N x heads x d_h")
+    if X.dtype != cache.K.dtype:
+        raise TypeError(f"{name} must have the cache's type")
+    if X.stride(2) != 1 or X.shape[1] > 1 and X.stride(1) != X.shape[2]:
+        raise ValueError(f"{name} must hold the heads of a token side by side")
+    return X.shape[0], X.shape[1], X.stride(0) if X.shape[0] > 1 else X.shape[1] * X.shape[2]
+
+
+def ada_cache_append(ctx: Context, cache: KVCache, K: torch.Tensor, V: torch.Tensor, off: torch.Tensor,
+                     length: torch.Tensor, len_out: Optional[torch.Tensor] = None, Q: Optional[torch.Tensor] = None,
+                     q_out: Optional[torch.Tensor] = None, q_norm: Optional[torch.Tensor] = None,
+                     k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                     inv_freq: Optional[torch.Tensor] = None, pos0: Optional[torch.Tensor] = None,
+                     rep_idx: Optional[torch.Tensor] = None, rep_cnt: Optional[torch.Tensor] = None, flags: int = 0,
+                     stream=None):
+    """Appends the new tokens' keys and values (N, h_kv, d_h) behind the `length` int32[B] tokens that the sequences
+    have; sequence b has rows off[b] .. off[b + 1].  Q (N, h, d_h) is normed and rotated alongside.  rep_idx, rep_cnt:
+    only these tokens are kept (the lists of a selection call).  Returns (q_out or None, len_out)."""
+    B = _ragged(cache, off, length)
+    N, hk, ldk = _rows_of(K, "K", cache)
+    _, hv, ldv = _rows_of(V, "V", cache, N)
+    if hk != cache.h_kv or hv != cache.h_kv:
+        raise ValueError("K and V must have the cache's heads")
+    if len_out is None:
+        len_out = torch.empty(B, dtype=torch.int32, device=K.device)
+    _int32(len_out, "len_out", B)
+    h = ldq = ldqo = 0
+    if Q is not None:
+        _, h, ldq = _rows_of(Q, "Q", cache, N)
+        if q_out is None:
+            q_out = torch.empty((N, h, cache.d_h), dtype=Q.dtype, device=Q.device)
+        _, ho, ldqo = _rows_of(q_out, "q_out", cache, N)
+        if ho != h:
+            raise ValueError("q_out must have Q's heads")
+    for w in (q_norm, k_norm):
+        if w is not None:
+            if w.dtype != K.dtype:
+                raise TypeError("the norms' weights must have the cache's type")
+            if w.shape != (cache.d_h,) or not w.is_contiguous():
+                raise ValueError("the norms' weights must be d_h dense elements")
+    if inv_freq is not None and (inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()):
+        raise TypeError("inv_freq must be a dense float64 vector")
+    if pos0 is not None:
+        _int32(pos0, "pos0", B)
+    if rep_idx is not None:
+        _int32(rep_idx, "rep_idx", N)
+    if rep_cnt is not None:
+        _int32(rep_cnt, "rep_cnt", B)
+    st = _fast.cache_append(ctx.addr, cache.addr, B, off, length, len_out, N, K, ldk, V, ldv, cache.dtype, Q, h, ldq, q_out,
+                            ldqo, q_norm, k_norm, eps, inv_freq, 0 if inv_freq is None else 2 * inv_freq.numel(), pos0,
+                            rep_idx, rep_cnt, flags, _stream_of(ctx, stream))
+    if st:
+        _raise(st, "ada_cache_append")
+    return q_out, len_out
+
+
+def ada_attention_cached(ctx: Context, cache: KVCache, Q: torch.Tensor, off: torch.Tensor, length: torch.Tensor,
+                         max_new: int, out: Optional[torch.Tensor] = None, scale: float = 0.0,
+                         flags: int = ADA_ATTN_CAUSAL, stream=None) -> torch.Tensor:
+    """Attention of new tokens Q (N, h, d_h) over their sequence's cache, whose `length` int32[B] counts them too;
+    max_new: the most new tokens that a sequence has.  Returns out (N, h, d_h) bf16; rows behind the last sequence are
+    left as they are (zeros in a fresh tensor)."""
+    B = _ragged(cache, off, length)
+    N, h, ldq = _rows_of(Q, "Q", cache)
+    if out is None:
+        out = torch.zeros((N, h, cache.d_h), dtype=Q.dtype, device=Q.device)
+    _, ho, ldo = _rows_of(out, "out", cache, N)
+    if ho != h:
+        raise ValueError("out must have Q's heads")
+    st = _fast.attention_cached(ctx.addr, cache.addr, B, off, length, N, max_new, Q, h, ldq, cache.dtype, scale, out, ldo,
+                                flags, _stream_of(ctx, stream))
+    if st:
+        _raise(st, "ada_attention_cached")
+    return out
+
+
+def _lists_of(cache: KVCache, N: int, blk_idx: torch.Tensor, blk_cnt: torch.Tensor, k: Optional[int] = None) -> int:
+    if blk_idx.dim() != 3 or blk_idx.shape[:2] != (N, cache.h_kv) or k is not None and blk_idx.shape[2] != k:
+        raise ValueError("blk_idx must be N x h_kv x k")
+    _int32(blk_idx, "blk_idx", blk_idx.numel())
+    _int32(blk_cnt, "blk_cnt", N * cache.h_kv)
+    return blk_idx.shape[2]
+
+
+def ada_select_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: torch.Tensor, length: torch.Tensor, k: int,
+                      n_first: int = 1, n_last: int = 1, blk_idx: Optional[torch.Tensor] = None,
+                      blk_cnt: Optional[torch.Tensor] = None, flags: int = ADA_ATTN_CAUSAL, stream=None):
+    """Per new token and key head the k pages with the largest bound of q . key.  Returns (blk_idx int32 (N, h_kv, k),
+    blk_cnt int32 (N, h_kv)); rows behind the last sequence are left as they are."""
+    B = _ragged(cache, off, length)
+    N, h, ldq = _rows_of(Q, "Q", cache)
+    if blk_idx is None:
+        blk_idx = torch.empty((N, cache.h_kv, k), dtype=torch.int32, device=Q.device)
+    if blk_cnt is None:
+        blk_cnt = torch.empty((N, cache.h_kv), dtype=torch.int32, device=Q.device)
+    _lists_of(cache, N, blk_idx, blk_cnt, k)
+    st = _fast.select_blocks(ctx.addr, cache.addr, B, off, length, N, Q, h, ldq, cache.dtype, k, n_first, n_last, blk_idx,
+                             blk_cnt, flags, _stream_of(ctx, stream))
+    if st:
+        _raise(st, "ada_select_blocks")
+    return blk_idx, blk_cnt
+
+
+def ada_attention_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: torch.Tensor, length: torch.Tensor,
+                         blk_idx: torch.Tensor, blk_cnt: torch.Tensor, out: Optional[torch.Tensor] = None,
+                         scale: float = 0.0, flags: int = ADA_ATTN_CAUSAL, stream=None) -> torch.Tensor:
+    """ada_attention_cached over the pages that blk_idx (N, h_kv, k), blk_cnt (N, h_kv) list."""
+    B = _ragged(cache, off, length)
+    N, h, ldq = _rows_of(Q, "Q", cache)
+    k = _lists_of(cache, N, blk_idx, blk_cnt)
+    if out is None:
+        out = torch.zeros((N, h, cache.d_h), dtype=Q.dtype, device=Q.device)
+    _, ho, ldo = _rows_of(out, "out", cache, N)
+    if ho != h:
+        raise ValueError("out must have Q's heads")
+    st = _fast.attention_blocks(ctx.addr, cache.addr, B, off, length, N, Q, h, ldq, cache.dtype, blk_idx, blk_cnt, k, scale,
+                                out, ldo, flags, _stream_of(ctx, stream))
+    if st:
+        _raise(st, "ada_attention_blocks")
     return out
 
 

@@ -18,7 +18,7 @@ NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-shared",
-    "-Xptxas", "-v", "-cudart", "static",
+    "-Xptxas", "-v", "-cudart", "static", "--threads", "0",
 ]
 
 

@@ -6,6 +6,7 @@
 #include <atomic>
 #include <new>
 
+#include "api_util.h"
 #include "common.cuh"
 
 using namespace ada;
@@ -20,8 +21,6 @@ const char* const kKernelNames[K_COUNT] = {
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 ada_status check_common(ada_ctx* ctx, const void* X, int64_t B, int64_t T, int64_t d, int64_t ldx,
                         ada_dtype dt) {
     if (ctx == nullptr || X == nullptr) return ADA_ERR_INVALID_ARG;
@@ -35,18 +34,6 @@ ada_status check_common(ada_ctx* ctx, const void* X, int64_t B, int64_t T, int64
 }
 
 inline bool tau_ok(double tau) { return tau > 0.0 && tau < 1.0; }  // also rejects NaN
-
-struct DeviceGuard {
-    int prev = -1;
-    explicit DeviceGuard(int dev) {
-        cudaGetDevice(&prev);
-        if (prev != dev) cudaSetDevice(dev);
-        else prev = -1;
-    }
-    ~DeviceGuard() {
-        if (prev >= 0) cudaSetDevice(prev);
-    }
-};
 
 bool use_tc(const ada_ctx* ctx, ada_dtype dt) {
     if (dt != ADA_BF16) return false;
@@ -80,16 +67,6 @@ bool use_pair(const ada_ctx* ctx, int64_t B, int64_t T, int64_t d, ada_dtype dt,
 
 // plane width of an fp32 row of d elements: whole 64-element K blocks
 inline int64_t plane_len(int64_t d) { return (d + 63) / 64 * 64; }
-
-
-#define CU(x)                                  \
-    do {                                       \
-        cudaError_t e__ = (x);                 \
-        if (e__ != cudaSuccess) {              \
-            cudaGetLastError(); /* reported by the status; the next launcher that asks must not find it */ \
-            return ADA_ERR_CUDA;               \
-        }                                      \
-    } while (0)
 
 }  // namespace
 
@@ -214,6 +191,7 @@ ada_status ada_create(ada_ctx** out, int device, int64_t maxB, int64_t maxT, int
     ctx->stage = nullptr; ctx->stage_bytes = 0; ctx->host_stream = nullptr;
     ctx->host_event = nullptr; ctx->host_ready = nullptr; ctx->host_out = false;
     ctx->attn_ws = nullptr; ctx->attn_ws_bytes = 0;
+    ctx->cache_ws = nullptr; ctx->cache_part = nullptr; ctx->cache_ctr = nullptr; ctx->cache_ctr_bytes = 0;
     ctx->map_cache = nullptr;
     ctx->tc_attr_set = false;
     ctx->cooperative = true;
@@ -295,6 +273,7 @@ ada_status ada_destroy(ada_ctx* ctx) {
     }
     if (ctx->stage) cudaFree(ctx->stage);
     if (ctx->attn_ws) cudaFree(ctx->attn_ws);
+    if (ctx->cache_ws) cudaFree(ctx->cache_ws);
     if (ctx->host_stream) cudaStreamDestroy(ctx->host_stream);
     if (ctx->host_event) cudaEventDestroy(ctx->host_event);
     if (ctx->host_ready) cudaEventDestroy(ctx->host_ready);
@@ -717,6 +696,7 @@ ada_status ada_device_status(ada_ctx* ctx, void* stream, int64_t* n_zero_norm_ro
         // a faulted call may have left scratch behind: restore the workspace invariants
         CU(cudaMemsetAsync(ctx->role, 0, (size_t)((char*)ctx->inv_norm - (char*)ctx->role), s));
         CU(cudaMemsetAsync(ctx->part_buf, 0xFF, ctx->part_bytes, s));
+        if (ctx->cache_ctr != nullptr) CU(cudaMemsetAsync(ctx->cache_ctr, 0, ctx->cache_ctr_bytes, s));
         if (ctx->g_rep_tok != nullptr) CU(cudaMemsetAsync(ctx->g_rep_tok, 0, (size_t)ctx->maxB * ctx->maxT * 4, s));
         CU(cudaStreamSynchronize(s));
     }

@@ -1,0 +1,601 @@
+// Attention of chunks of new tokens over the paged cache (ada_attention_cached) on the 5th-generation tensor cores.
+//
+// The same softmax(scale q K^T) V in one pass over the keys as in cache_step.cu, for as many rows as a tile holds:
+// the G heads that share a key head times 128 / G consecutive tokens are the 128 rows of a tile, two tiles (512 columns
+// of TMEM: two score tiles, two accumulators) are a CTA's work item, and both read the same tiles of 128 keys.
+//   warp 0      TMA: queries, and pages of K and V into a ring of slots (one slot = K or V of 128 keys)
+//   warp 1      tcgen05.mma: S_t = Q_t K^T, O_t += P_t V; while tile 0's softmax runs, tile 1's products do
+//   warps 2..5  softmax of tile 0, one row per thread: S out of TMEM into registers, 2^(s - m), P back into TMEM as bf16
+//               over its own scores, where the second product takes it from as its left operand
+//   warps 6..9  the same for tile 1
+// V needs no transposed copy: its tiles are MN-major right operands as the pages hold them.
+// A row's reference maximum m is raised only when the running maximum has left it by more than 8 powers of two
+// (then the accumulator is rescaled in TMEM); O / l does not depend on it.
+//
+// Work: items (sequence, 2 x 128 / G tokens, key head) cost as many units as they see key tiles; every CTA takes an
+// equal run of units.  An item that several CTAs share is joined, 32 rows at a time, by the warp that finishes last,
+// in the order of the keys; nobody waits for another CTA.
+#include "cache_tma.cuh"
+
+namespace ada {
+
+using namespace tc;
+
+namespace {
+
+constexpr int CH_THREADS = 320;
+constexpr int CH_KEYS = 128;                      // keys per tile
+constexpr int BLK_BYTES = 128 * BK * 2;           // 128 rows x 64 elements: 16 KiB
+constexpr float CH_LAG = 8.0f;
+constexpr int PART_FLOATS = 256 * 128 + 2 * 256;  // one item's partial result: columns x rows, maxima, sums
+
+template <int NDB> __host__ __device__ constexpr int ch_slots() { return 10 / NDB; }
+
+struct ChunkShared {
+    unsigned long long q_full, q_empty, full[10], empty[10], s_full[2], p_full[2], o_full[2], o_empty[2];
+    unsigned tmem_base;
+    int abort_flag[2];
+    int start[4];                                 // b, p, head, ku of the CTA's first unit
+    long long range[3];                           // first unit, one past the last, units per CTA
+};
+template <int NDB> __host__ __device__ constexpr int ch_smem() { return 14 * BLK_BYTES + (int)sizeof(ChunkShared); }
+static_assert(ch_smem<2>() <= 227 * 1024, "shared memory budget");
+
+struct ChunkMaps {
+    CUtensorMap q, k, v;
+};
+
+struct Item {
+    int b, head, row0, n_tok;             // first token's row; tokens of both tiles
+    int first_lim;                        // keys that the first token sees
+    int kv;                               // the sequence's length: keys behind it are nobody's
+    int units[2];                         // key tiles of either tile of rows (0: no rows)
+    int ku, take;                         // the CTA's units of it
+    int pieces, piece, c0, c1;
+};
+
+// tq tokens per row tile
+struct ChunkWork {
+    long long at, end, per;
+    int b, p, head, ku;
+    int n, off, len, nu, P;
+
+    static __device__ __forceinline__ int limit(int n, int len, int tok, int causal) {   // keys that the tokens below `tok` see
+        return max(causal ? len - n + min(tok, n) : len, 0);
+    }
+    static __device__ __forceinline__ int units(int n, int len, int p, int tq, int causal) {
+        return max((limit(n, len, (p + 1) * 2 * tq, causal) + CH_KEYS - 1) / CH_KEYS, 1);
+    }
+    __device__ __forceinline__ void load_seq(const Ragged& r, const CacheView& c, int tq, int max_new) {
+        n = seq_rows(r, b, off);
+        len = seq_len(r, c, b);
+        P = (min(n, max_new) + 2 * tq - 1) / (2 * tq);
+    }
+    __device__ __forceinline__ bool next(Item& it, const Ragged& r, const CacheView& c, int tq, int causal, int max_new) {
+        if (at >= end) return false;
+        while (P == 0 || ku >= nu) {
+            ku = 0;
+            if (P == 0 || ++head >= c.h_kv) {
+                head = 0;
+                if (P == 0 || ++p >= P) {
+                    p = 0;
+                    if (++b >= r.B) { at = end; return false; }
+                    load_seq(r, c, tq, max_new);
+                    if (P == 0) continue;
+                }
+                nu = units(n, len, p, tq, causal);
+            }
+        }
+        const int t0 = p * 2 * tq;
+        it.b = b; it.head = head; it.row0 = off + t0;
+        it.n_tok = min(min(n, max_new) - t0, 2 * tq);
+        it.first_lim = causal ? len - n + t0 + 1 : len;
+        it.kv = len;
+        it.units[0] = min((limit(n, len, t0 + tq, causal) + CH_KEYS - 1) / CH_KEYS, nu);
+        it.units[1] = it.n_tok > tq ? nu : 0;
+        it.ku = ku;
+        it.take = (int)min((long long)(nu - ku), end - at);
+        const long long first = at - ku;
+        it.c0 = (int)(first / per);
+        it.c1 = (int)((first + nu - 1) / per);
+        it.pieces = it.c1 - it.c0 + 1;
+        it.piece = (int)(at / per) - it.c0;
+        at += it.take; ku += it.take;
+        return true;
+    }
+    // key tiles of row tile t in this CTA's share of the item
+    static __device__ __forceinline__ int tiles_of(const Item& it, int t) { return max(min(it.units[t] - it.ku, it.take), 0); }
+};
+
+// O += P V with P in TMEM: 16 keys per instruction, V as an MN-major tile (64-element blocks of 128 keys x 128 bytes)
+__device__ __forceinline__ void umma_ts(unsigned tmem_d, unsigned tmem_a, unsigned long long bdesc, unsigned idesc,
+                                        unsigned accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// MN-major tile, 128-byte swizzle: 8 keys are 1024 bytes, the next 64 elements of a row BLK_BYTES further on
+__device__ __forceinline__ unsigned long long smem_desc_mn(unsigned addr) {
+    unsigned long long d = 0;
+    d |= (unsigned long long)((addr & 0x3FFFFu) >> 4);
+    d |= (unsigned long long)(BLK_BYTES >> 4) << 16;
+    d |= (unsigned long long)(1024 >> 4) << 32;
+    d |= (unsigned long long)1 << 46;
+    d |= (unsigned long long)2 << 61;
+    return d;
+}
+
+template <int NDB>
+__global__ void __launch_bounds__(CH_THREADS, 1)
+k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const Ragged r, const AttendJob j, int tq,
+              float* __restrict__ ws, unsigned* __restrict__ counters, unsigned* __restrict__ status) {
+    constexpr int SLOTS = ch_slots<NDB>();
+    constexpr int SLOT_BYTES = NDB * BLK_BYTES;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    unsigned char* qs = smem;                              // two tiles of queries
+    unsigned char* ring = smem + 2 * NDB * BLK_BYTES;
+    ChunkShared& sh = *reinterpret_cast<ChunkShared*>(smem + 14 * BLK_BYTES);
+    volatile int* abort_flag = sh.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int G = j.h / c.h_kv;
+    if ((smem_u32(smem) & 1023u) != 0u) {
+        grid_dep_wait();
+        if (threadIdx.x == 0) { atomicOr(status, ST_TIMEOUT); status[2] = 499u; }
+        return;
+    }
+    if (threadIdx.x == 0) {
+        mbar_init(&sh.q_full, 1); mbar_init(&sh.q_empty, 1);
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&sh.s_full[t], 1); mbar_init(&sh.p_full[t], 4);
+            mbar_init(&sh.o_full[t], 1); mbar_init(&sh.o_empty[t], 4);
+        }
+        sh.abort_flag[0] = 0;
+        sh.abort_flag[1] = wait_limit_units(false);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32(&sh.tmem_base)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (threadIdx.x == 64) { prefetch_map(&maps.q); prefetch_map(&maps.k); prefetch_map(&maps.v); }
+    grid_dep_wait();
+    grid_dep_launch_next();
+    if (warp == 0) {
+        // every CTA's first unit: units of all sequences, 32 at a time (a lane adds up the items of its own)
+        auto units_of = [&](int b) {
+            if (b >= r.B) return 0;
+            int o;
+            const int n = seq_rows(r, b, o), len = seq_len(r, c, b);
+            if (blockIdx.x == 0 && n > j.max_new) atomicOr(status, ST_BAD_COUNT);
+            const int P = (min(n, j.max_new) + 2 * tq - 1) / (2 * tq);
+            int u = 0;
+            for (int p = 0; p < P; ++p) u += ChunkWork::units(n, len, p, tq, j.causal);
+            return u;
+        };
+        long long U = 0;
+        int first = 0;
+        for (int b0 = 0; b0 < r.B; b0 += 32) {
+            const int u = units_of(b0 + lane);
+            if (b0 == 0) first = u;
+            unsigned long long x = (unsigned long long)u;
+#pragma unroll
+            for (int m = 16; m > 0; m >>= 1) x += __shfl_xor_sync(0xffffffffu, x, m);
+            U += (long long)x;
+        }
+        U *= c.h_kv;
+        const long long per = max((U + gridDim.x - 1) / gridDim.x, 1ll);
+        const long long at = min(per * blockIdx.x, U), end = min(at + per, U);
+        int b = 0, p = 0, head = 0, ku = 0;
+        long long before = 0;
+        if (at < end)
+            for (int b0 = 0; b0 < r.B; b0 += 32) {
+                const int own = b0 == 0 ? first : units_of(b0 + lane);
+                long long sum = own;
+#pragma unroll
+                for (int m = 1; m < 32; m <<= 1) {
+                    const long long y = __shfl_up_sync(0xffffffffu, sum, m);
+                    if (lane >= m) sum += y;
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, at < (before + sum) * c.h_kv);
+                if (hit != 0u) {
+                    const int l = __ffs(hit) - 1;
+                    before += __shfl_sync(0xffffffffu, sum - own, l);
+                    b = b0 + l;
+                    int o;
+                    const int n = seq_rows(r, b, o), len = seq_len(r, c, b);
+                    long long rest = at - before * c.h_kv;
+                    int u = ChunkWork::units(n, len, 0, tq, j.causal);
+                    while (rest >= (long long)u * c.h_kv) {
+                        rest -= (long long)u * c.h_kv;
+                        ++p;
+                        u = ChunkWork::units(n, len, p, tq, j.causal);
+                    }
+                    head = (int)(rest / u);
+                    ku = (int)(rest % u);
+                    break;
+                }
+                before += __shfl_sync(0xffffffffu, sum, 31);
+            }
+        if (lane == 0) {
+            sh.start[0] = b; sh.start[1] = p; sh.start[2] = head; sh.start[3] = ku;
+            sh.range[0] = at; sh.range[1] = end; sh.range[2] = per;
+        }
+    } else if (blockIdx.x == 0 && warp == 2) {
+        check_ragged(r, c, status, lane, 32);
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const unsigned tmem_base = sh.tmem_base;
+    ChunkWork work;
+    work.at = sh.range[0]; work.end = sh.range[1]; work.per = sh.range[2];
+    work.b = sh.start[0]; work.p = sh.start[1]; work.head = sh.start[2]; work.ku = sh.start[3];
+    work.n = work.off = work.len = work.nu = work.P = 0;
+    if (work.at < work.end) {
+        work.load_seq(r, c, tq, j.max_new);
+        work.nu = ChunkWork::units(work.n, work.len, work.p, tq, j.causal);
+    }
+    Item it;
+
+    if (warp == 0) {
+        // ------------------------------------------------ TMA producer
+        bool ok = true;
+        unsigned put = 0;                          // slots filled: K, V, K, V ...
+        const int np = CH_KEYS >> min(c.shift, 7); // pages per key tile
+        const int ps = 1 << c.shift;
+        int k = 0;                                 // items
+        for (; ok && work.next(it, r, c, tq, j.causal, j.max_new); ++k) {
+            if (k > 0) ok = mbar_wait(&sh.q_empty, (unsigned)(k - 1) & 1u, abort_flag, 30);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;                        // (k items' queries have been asked for)
+            const int two = it.units[1] > 0 ? 2 : 1;
+            if (lane == 0) {
+                mbar_expect_tx(&sh.q_full, (unsigned)(two * NDB * tq * G * 128));
+                for (int t = 0; t < two; ++t)
+                    for (int db = 0; db < NDB; ++db)
+                        tma_load_4d(&maps.q, &sh.q_full, qs + (t * NDB + db) * BLK_BYTES, db * BK, 0, it.head, it.row0 + t * tq);
+            }
+            int page = -1, batch = -1;             // lane l: the sequence's page batch + l
+            const int pages = (it.kv + ps - 1) >> c.shift;
+            for (int u = 0; u < it.take && ok; ++u) {
+                const int p0 = (it.ku + u) * np;
+                if (batch < 0 || p0 + np > batch + 32) {
+                    batch = p0;
+                    page = p0 + lane < pages ? page_of(c, it.b, p0 + lane, status) : -1;
+                }
+                const int mine = __shfl_sync(0xffffffffu, page, (p0 - batch + lane) & 31);
+                const bool have = lane < np && mine >= 0;
+                const unsigned bytes = (unsigned)__popc(__ballot_sync(0xffffffffu, have)) * (unsigned)(ps * 128 * NDB);
+                for (int kv = 0; kv < 2 && ok; ++kv, ++put) {
+                    const int st = put % SLOTS;
+                    ok = mbar_wait(&sh.empty[st], ((put / SLOTS) & 1u) ^ 1u, abort_flag, 31);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(&sh.full[st], bytes);
+                    __syncwarp();
+                    if (have)
+                        for (int db = 0; db < NDB; ++db)
+                            tma_load_4d(kv == 0 ? &maps.k : &maps.v, &sh.full[st],
+                                        ring + st * SLOT_BYTES + db * BLK_BYTES + lane * ps * 128, db * BK, 0, it.head, mine);
+                }
+            }
+        }
+        // every copy has to land before the CTA may exit
+        if (lane == 0) {
+            const unsigned long long t0 = global_ns();
+            while (k > 0 && !mbar_try(&sh.q_full, (unsigned)(k - 1) & 1u))
+                if (past_limit(2 * (global_ns() - t0), abort_flag)) { *abort_flag = 33; break; }
+            for (unsigned i = put > (unsigned)SLOTS ? put - SLOTS : 0u; i < put; ++i)
+                while (!mbar_try(&sh.full[i % SLOTS], (i / SLOTS) & 1u))
+                    if (past_limit(2 * (global_ns() - t0), abort_flag)) { *abort_flag = 33; break; }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA issuer (lane 0; all lanes follow)
+        bool ok = true;
+        unsigned got = 0;                          // slots consumed
+        unsigned n_p[2] = {0u, 0u}, n_o[2] = {0u, 0u};
+        const unsigned idesc_s = instr_desc(CH_KEYS);
+        const unsigned idesc_o = instr_desc(NDB * 64) | (1u << 16);          // right operand MN-major
+        for (int k = 0; ok && work.next(it, r, c, tq, j.causal, j.max_new); ++k) {
+            const int nt[2] = {ChunkWork::tiles_of(it, 0), ChunkWork::tiles_of(it, 1)};
+            const int two = it.units[1] > 0 ? 2 : 1;
+            ok = mbar_wait(&sh.q_full, (unsigned)k & 1u, abort_flag, 35);
+            auto wait_slot = [&](unsigned i, int where) {
+                ok = ok && mbar_wait(&sh.full[i % SLOTS], (i / SLOTS) & 1u, abort_flag, where);
+                ok = __all_sync(0xffffffffu, ok);
+            };
+            auto issue_s = [&](int t, unsigned slot) {
+                const unsigned long long a = smem_desc_sw128(smem_u32(qs + t * NDB * BLK_BYTES));
+                const unsigned long long b = smem_desc_sw128(smem_u32(ring + (slot % SLOTS) * SLOT_BYTES));
+                umma_blocks<NDB>(tmem_base + t * 128, a, b, BLK_BYTES, BLK_BYTES, idesc_s);
+                umma_commit(&sh.s_full[t]);
+            };
+            wait_slot(got, 36);
+            if (!ok) break;
+            tcgen05_fence_after();
+            if (lane == 0) {
+                for (int t = 0; t < two; ++t)
+                    if (nt[t] > 0) issue_s(t, got);
+                umma_commit(&sh.empty[got % SLOTS]);
+                if (it.take == 1) umma_commit(&sh.q_empty);
+            }
+            for (int u = 0; u < it.take && ok; ++u, got += 2) {
+                const unsigned sv = got + 1, sk = got + 2;
+                wait_slot(sv, 38);
+                if (!ok) break;
+                // values of slots behind the sequence's length meet probabilities of zero: they must not be NaN
+                const int live = it.kv - (it.ku + u) * CH_KEYS;
+                if (live < CH_KEYS) {
+                    unsigned char* v = ring + (sv % SLOTS) * SLOT_BYTES;
+                    for (int q = max(live, 0) * 8 + lane; q < CH_KEYS * 8; q += 32)
+#pragma unroll
+                        for (int db = 0; db < NDB; ++db)
+                            *reinterpret_cast<uint4*>(v + db * BLK_BYTES + q * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+                const bool ahead = u + 1 < it.take;
+                if (ahead) wait_slot(sk, 37);
+                if (!ok) break;
+                for (int t = 0; t < two; ++t) {
+                    if (u >= nt[t]) continue;
+                    ok = mbar_wait(&sh.p_full[t], n_p[t] & 1u, abort_flag, 39);
+                    ++n_p[t];
+                    // the accumulator is overwritten: the previous item's rows have been read out
+                    if (u == 0 && n_o[t] > 0) ok = ok && mbar_wait(&sh.o_empty[t], (n_o[t] - 1u) & 1u, abort_flag, 40);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tcgen05_fence_after();
+                    if (lane == 0) {
+                        const unsigned long long b = smem_desc_mn(smem_u32(ring + (sv % SLOTS) * SLOT_BYTES));
+#pragma unroll
+                        for (int q = 0; q < CH_KEYS / UMMA_K; ++q)
+                            umma_ts(tmem_base + 256 + t * 128, tmem_base + t * 128 + q * 8, b + q * (2048 >> 4), idesc_o, (u | q) != 0);
+                        if (u + 1 < nt[t]) issue_s(t, sk);
+                        else umma_commit(&sh.o_full[t]);
+                    }
+                    if (u + 1 >= nt[t]) ++n_o[t];
+                }
+                if (!ok) break;
+                if (lane == 0) {
+                    umma_commit(&sh.empty[sv % SLOTS]);
+                    if (ahead) umma_commit(&sh.empty[sk % SLOTS]);
+                    if (u + 2 == it.take) umma_commit(&sh.q_empty);   // the item's last scores are under way
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------ softmax and output
+        const int quad = warp & 3, t = (warp - 2) >> 2;
+        const int i = quad * 32 + lane;                                     // row of the tile
+        const unsigned t_s = tmem_base + ((unsigned)(quad * 32) << 16) + t * 128;
+        const unsigned t_o = t_s + 256;
+        const int tok = i / G, g = i - tok * G;                             // within the tile
+        bool ok = true;
+        unsigned n_s = 0, n_o = 0;
+        while (work.next(it, r, c, tq, j.causal, j.max_new)) {
+            if (it.units[t] == 0 && t == 1) continue;                       // no rows in this tile
+            const int nt = ChunkWork::tiles_of(it, t);
+            const int tok_i = t * tq + tok;                                 // within the item
+            const bool live = tok < tq && tok_i < it.n_tok;
+            const int lim = !live ? 0 : j.causal ? min(it.first_lim + tok_i, it.kv) : it.kv;
+            const int lim_tile = j.causal ? it.first_lim + t * tq : it.kv;   // smallest of the tile's live rows
+            float m = -INFINITY, l = 0.f;
+            for (int u = 0; u < nt; ++u) {
+                if (ok) ok = mbar_wait(&sh.s_full[t], n_s & 1u, abort_flag, 41);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ++n_s;
+                tcgen05_fence_after();
+                unsigned x[4][32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_ld32_issue(t_s + q * 32, x[q]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_ld_wait(x[q]);
+                const int k0 = (it.ku + u) * CH_KEYS;
+                if (k0 + CH_KEYS > lim_tile) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (k0 + q * 32 + e >= lim) x[q][e] = 0xff800000u;
+                }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(x[q][e]));
+                const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * j.scale);
+                if (u == 0) {
+                    m = m_new;
+                } else {
+                    const bool raise = m_new > m + CH_LAG;
+                    if (__any_sync(0xffffffffu, raise)) {
+                        // (the scores' barrier also says that the previous tile's product is done)
+                        const float f = raise ? (m > -INFINITY ? ex2_approx(m - m_new) : 0.f) : 1.0f;
+#pragma unroll
+                        for (int q = 0; q < NDB * 2; ++q) {
+                            unsigned y[32];
+                            tmem_ld32_issue(t_o + q * 32, y);
+                            tmem_ld_wait(y);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+                            tmem_st32(t_o + q * 32, y);
+                        }
+                        l *= f;
+                        if (raise) m = m_new;
+                    }
+                }
+                const float ref = m > -INFINITY ? m : 0.f;
+                float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+                for (int h2 = 0; h2 < 2; ++h2) {
+                    unsigned w[32];
+#pragma unroll
+                    for (int e = 0; e < 64; e += 4) {
+                        const float p0 = ex2_approx(fmaf(__uint_as_float(x[2 * h2 + (e >> 5)][e & 31]), j.scale, -ref));
+                        const float p1 = ex2_approx(fmaf(__uint_as_float(x[2 * h2 + (e >> 5)][(e & 31) + 1]), j.scale, -ref));
+                        const float p2 = ex2_approx(fmaf(__uint_as_float(x[2 * h2 + (e >> 5)][(e & 31) + 2]), j.scale, -ref));
+                        const float p3 = ex2_approx(fmaf(__uint_as_float(x[2 * h2 + (e >> 5)][(e & 31) + 3]), j.scale, -ref));
+                        s0 += p0; s1 += p1; s2 += p2; s3 += p3;
+                        const __nv_bfloat162 lo = __floats2bfloat162_rn(p0, p1), hi = __floats2bfloat162_rn(p2, p3);
+                        w[e >> 1] = *reinterpret_cast<const unsigned*>(&lo);
+                        w[(e >> 1) + 1] = *reinterpret_cast<const unsigned*>(&hi);
+                    }
+                    tmem_st32(t_s + h2 * 32, w);
+                }
+                l += (s0 + s1) + (s2 + s3);
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.p_full[t]);
+            }
+            if (!ok) break;
+            // ---- the item's rows
+            if (nt > 0) {
+                ok = mbar_wait(&sh.o_full[t], n_o & 1u, abort_flag, 43);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                ++n_o;
+                tcgen05_fence_after();
+            }
+            __nv_bfloat16* dst = j.out + (int64_t)(it.row0 + tok_i) * j.ldo + ((int64_t)it.head * G + g) * c.d;
+            if (it.pieces == 1) {
+                const float f = l > 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+                for (int q = 0; q < NDB * 2; ++q) {
+                    unsigned y[32];
+                    if (nt > 0) { tmem_ld32_issue(t_o + q * 32, y); tmem_ld_wait(y); }
+                    else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) y[e] = 0u;
+                    }
+                    if (live) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            if (q * 32 + e < c.d) {
+                                unsigned w[4];
+#pragma unroll
+                                for (int v = 0; v < 4; ++v) {
+                                    const __nv_bfloat162 p = __floats2bfloat162_rn(__uint_as_float(y[e + 2 * v]) * f, __uint_as_float(y[e + 2 * v + 1]) * f);
+                                    w[v] = *reinterpret_cast<const unsigned*>(&p);
+                                }
+                                *reinterpret_cast<uint4*>(dst + q * 32 + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                            }
+                    }
+                }
+            } else {
+                // a share of an item: unnormalised, columns x rows (a warp's lanes write next to each other)
+                auto part = [&](int piece) { return ws + (2 * (int64_t)(it.c0 + piece) + (piece == 0 ? 1 : 0)) * PART_FLOATS; };
+                float* mine = part(it.piece) + t * 128 + i;
+#pragma unroll
+                for (int q = 0; q < NDB * 2; ++q) {
+                    unsigned y[32];
+                    if (nt > 0) { tmem_ld32_issue(t_o + q * 32, y); tmem_ld_wait(y); }
+                    else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) y[e] = 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) __stcg(mine + (q * 32 + e) * 256, __uint_as_float(y[e]));
+                }
+                __stcg(mine + 128 * 256, m);
+                __stcg(mine + 128 * 256 + 256, l);
+                __threadfence();
+                __syncwarp();
+                unsigned last = 0u;
+                if (lane == 0) {
+                    unsigned* ctr = counters + ((size_t)it.c1 * 2 + t) * 4 + quad;
+                    last = atomicAdd(ctr, 1u) + 1u == (unsigned)it.pieces;
+                    if (last) *ctr = 0u;                                     // as the next call finds it
+                }
+                last = __shfl_sync(0xffffffffu, last, 0);
+                if (last) {
+                    __threadfence();
+                    float M = -INFINITY, L = 0.f;
+                    for (int p = 0; p < it.pieces; ++p) M = fmaxf(M, __ldcg(part(p) + t * 128 + i + 128 * 256));
+                    const float Mr = M > -INFINITY ? M : 0.f;
+                    for (int p = 0; p < it.pieces; ++p) {
+                        const float* o = part(p) + t * 128 + i + 128 * 256;
+                        L = fmaf(__ldcg(o + 256), ex2_approx(__ldcg(o) - Mr), L);
+                    }
+                    const float f = L > 0.f ? 1.0f / L : 0.f;
+                    for (int q = 0; q < NDB * 8; ++q) {
+                        if (q * 8 >= c.d) break;
+                        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                        for (int p = 0; p < it.pieces; ++p) {
+                            const float* o = part(p) + t * 128 + i;
+                            const float fp = ex2_approx(__ldcg(o + 128 * 256) - Mr);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) y[e] = fmaf(__ldcg(o + (q * 8 + e) * 256), fp, y[e]);
+                        }
+                        if (live) {
+                            unsigned w[4];
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) {
+                                const __nv_bfloat162 p = __floats2bfloat162_rn(y[2 * v] * f, y[2 * v + 1] * f);
+                                w[v] = *reinterpret_cast<const unsigned*>(&p);
+                            }
+                            *reinterpret_cast<uint4*>(dst + q * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                }
+            }
+            tcgen05_fence_before();
+            __syncwarp();
+            if (nt > 0 && lane == 0) mbar_arrive(&sh.o_empty[t]);
+        }
+        tcgen05_fence_before();
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tcgen05_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+    }
+    if (threadIdx.x == 0 && sh.abort_flag[0] != 0) {
+        atomicOr(status, ST_TIMEOUT);
+        status[2] = 400u + (unsigned)sh.abort_flag[0];
+    }
+}
+
+// queries as (element, head of the group, key head, token): a box is 64 elements of G heads x tq tokens
+bool encode_queries(CUtensorMap* map, const CacheView& c, const Ragged& r, const AttendJob& j, int G, int tq) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)c.d, (cuuint64_t)G, (cuuint64_t)c.h_kv, (cuuint64_t)r.N};
+    const cuuint64_t strides[3] = {(cuuint64_t)c.d * 2, (cuuint64_t)G * c.d * 2, (cuuint64_t)j.ldq * 2};
+    const cuuint32_t box[4] = {(cuuint32_t)BK, (cuuint32_t)G, 1, (cuuint32_t)tq};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<__nv_bfloat16*>(j.Q), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NDB>
+cudaError_t run_chunk(ada_ctx* ctx, const ChunkMaps& maps, const CacheView& c, const Ragged& r, const AttendJob& j, int tq,
+                      cudaStream_t s) {
+    cudaError_t e = cudaFuncSetAttribute(k_cache_chunk<NDB>, cudaFuncAttributeMaxDynamicSharedMemorySize, ch_smem<NDB>());
+    if (e != cudaSuccess) return e;
+    return launch_k(ctx, k_cache_chunk<NDB>, dim3(ctx->sm_count), dim3(CH_THREADS), ch_smem<NDB>(), s, maps, c, r, j, tq,
+                    ctx->cache_part, ctx->cache_ctr, ctx->status);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_chunk(ada_ctx* ctx, const CacheView& c, const Ragged& r, const AttendJob& j, cudaStream_t s) {
+    const int G = j.h / c.h_kv, tq = 128 / G;
+    const int ps = 1 << c.shift;
+    ChunkMaps maps;
+    if (!encode_pages(&maps.k, c, c.k, ps < 128 ? ps : 128) || !encode_pages(&maps.v, c, c.v, ps < 128 ? ps : 128) ||
+        !encode_queries(&maps.q, c, r, j, G, tq))
+        return cudaErrorInvalidValue;
+    return c.d > 64 ? run_chunk<2>(ctx, maps, c, r, j, tq, s) : run_chunk<1>(ctx, maps, c, r, j, tq, s);
+}
+
+size_t cache_part_floats() { return (size_t)PART_FLOATS; }
+
+}  // namespace ada

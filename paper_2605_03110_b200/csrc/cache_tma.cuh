@@ -1,0 +1,41 @@
+// TMA access to the pages of a cache and to the new tokens' queries: maps, loads, warp-level matrix instructions.
+#pragma once
+
+#include "cache_dev.cuh"
+#include "gram_tc_dev.cuh"
+
+namespace ada {
+namespace tc {
+
+static __device__ __forceinline__ void tma_load_4d(const CUtensorMap* map, unsigned long long* bar, void* dst, int c0,
+                                                   int c1, int c2, int c3) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<unsigned long long>(map)), "r"(smem_u32(bar)), "r"(c0), "r"(c1),
+          "r"(c2), "r"(c3)
+        : "memory");
+}
+
+static __device__ __forceinline__ float ex2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// (element, slot, head, page): boxes of 64 elements x `box_rows` slots of one head and page, 128-byte swizzle
+static inline bool encode_pages(CUtensorMap* map, const CacheView& c, const void* base, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) return false;
+    const int ps = 1 << c.shift;
+    const cuuint64_t dims[4] = {(cuuint64_t)c.d, (cuuint64_t)ps, (cuuint64_t)c.h_kv, (cuuint64_t)c.n_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)c.d * 2, (cuuint64_t)ps * c.d * 2, (cuuint64_t)c.page_stride * 2};
+    const cuuint32_t box[4] = {(cuuint32_t)BK, (cuuint32_t)box_rows, 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace tc
+}  // namespace ada

@@ -207,6 +207,12 @@ struct ada_ctx {
     // gathered Q_R, K_R, V_R^T of the attention on the representative set (allocated on first use)
     char* attn_ws;
     size_t attn_ws_bytes;
+    // attention over a paged cache (allocated on first use, of one size): partial results of rows that several CTAs
+    // share, and how many of them are there (all zero between calls)
+    char* cache_ws;
+    float* cache_part;
+    unsigned* cache_ctr;
+    size_t cache_ctr_bytes;
     void* map_cache;     // tc::MapCache, or NULL: none kept
     // staging for the *_host entry points (allocated on first use)
     char* stage;

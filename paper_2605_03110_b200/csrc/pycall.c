@@ -104,10 +104,42 @@ static PyObject* attention_reps(PyObject* self, PyObject* const* a, Py_ssize_t n
     CALL(ada_attention_reps(c, Q, K, V, T, h, dh, ld, (ada_dtype)dt, ri, ric, near, out, ldo, (uint32_t)flags, s));
 }
 
+static PyObject* cache_append(PyObject* self, PyObject* const* a, Py_ssize_t na) {
+    ARGS(27);
+    H(ada_ctx, c); H(ada_kv_cache, kv); N(B); P(int32_t, off); P(int32_t, len); O(int32_t, len_out); N(rows);
+    P(void, K); N(ldk); P(void, V); N(ldv); N(dt); O(void, Q); N(h); N(ldq); O(void, q_out); N(ldqo);
+    O(void, q_norm); O(void, k_norm); D(eps); O(double, inv_freq); N(rot); O(int32_t, pos0); O(int32_t, ri);
+    O(int32_t, ric); N(flags); H(void, s);
+    CALL(ada_cache_append(c, kv, B, off, len, len_out, rows, K, ldk, V, ldv, (ada_dtype)dt, Q, h, ldq, q_out, ldqo,
+                          q_norm, k_norm, eps, inv_freq, rot, pos0, ri, ric, (uint32_t)flags, s));
+}
+static PyObject* attention_cached(PyObject* self, PyObject* const* a, Py_ssize_t na) {
+    ARGS(16);
+    H(ada_ctx, c); H(ada_kv_cache, kv); N(B); P(int32_t, off); P(int32_t, len); N(rows); N(max_new); P(void, Q); N(h);
+    N(ldq); N(dt); D(scale); P(void, out); N(ldo); N(flags); H(void, s);
+    CALL(ada_attention_cached(c, kv, B, off, len, rows, max_new, Q, h, ldq, (ada_dtype)dt, scale, out, ldo,
+                              (uint32_t)flags, s));
+}
+static PyObject* select_blocks(PyObject* self, PyObject* const* a, Py_ssize_t na) {
+    ARGS(17);
+    H(ada_ctx, c); H(ada_kv_cache, kv); N(B); P(int32_t, off); P(int32_t, len); N(rows); P(void, Q); N(h); N(ldq); N(dt);
+    N(k_); N(first); N(last); P(int32_t, bi); P(int32_t, bc); N(flags); H(void, s);
+    CALL(ada_select_blocks(c, kv, B, off, len, rows, Q, h, ldq, (ada_dtype)dt, k_, first, last, bi, bc, (uint32_t)flags,
+                           s));
+}
+static PyObject* attention_blocks(PyObject* self, PyObject* const* a, Py_ssize_t na) {
+    ARGS(18);
+    H(ada_ctx, c); H(ada_kv_cache, kv); N(B); P(int32_t, off); P(int32_t, len); N(rows); P(void, Q); N(h); N(ldq); N(dt);
+    P(int32_t, bi); P(int32_t, bc); N(k_); D(scale); P(void, out); N(ldo); N(flags); H(void, s);
+    CALL(ada_attention_blocks(c, kv, B, off, len, rows, Q, h, ldq, (ada_dtype)dt, bi, bc, k_, scale, out, ldo,
+                              (uint32_t)flags, s));
+}
+
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(select_full), METHOD(select_full_heads), METHOD(cascade_step),
                                 METHOD(cascade_step_heads), METHOD(cascade_step_adaptive), METHOD(nearest_rep),
-                                METHOD(attention_reps), {NULL, NULL, 0, NULL}};
+                                METHOD(attention_reps), METHOD(cache_append),
+                                METHOD(attention_cached), METHOD(select_blocks), METHOD(attention_blocks), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", NULL, -1, methods};
 
 PyMODINIT_FUNC PyInit__pycall(void) {
