@@ -7,9 +7,10 @@
 // far positions, where an fp32 product knows nothing of the angle any more); sine and cosine of the fraction are fp32.
 // One rounding to bf16, at the store.
 //
-// Bound by memory (2 bytes in, 2 out per element), for single tokens by latency.  A group of 16 (d_h <= 64: 8) lanes
-// holds one head's row, 8 elements a lane, so that norm and rotation are shuffles inside the group; a token's
-// sines and cosines are made once per block and shared by all of its heads.
+// Bound by memory (2 bytes in, 2 out per element), for single tokens by latency.  A warp has one token (or a share of its
+// heads), half a warp (d_h <= 64: a quarter) one head's row at a time.  A lane holds two pieces of four elements that the
+// rotation pairs with each other, so that it needs nobody else's elements, and keeps the four sines and cosines of
+// its pairs, and the norm's weights, in registers for all heads of the token.
 #include "cache_dev.cuh"
 
 namespace ada {
@@ -17,196 +18,110 @@ namespace ada {
 namespace {
 
 constexpr int APP_THREADS = 256;
+constexpr int APP_WARPS = APP_THREADS / 32;
 constexpr int APP_ROWS = 4;              // rows of a group in flight
-constexpr int APP_TOK = 4;               // most tokens per block
-constexpr int MAX_HALF = 64;             // rot / 2 <= 64
-
-struct TokInfo {
-    int page, slot, src, bad;            // page -1: nothing is kept of this row
-};
 
 // bf16 pairs with an exponent of all ones
 __device__ __forceinline__ bool nonfinite2(unsigned w) {
     return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
-__device__ __forceinline__ bool nonfinite8(const uint4& v) {
-    return nonfinite2(v.x) || nonfinite2(v.y) || nonfinite2(v.z) || nonfinite2(v.w);
+__device__ __forceinline__ bool nonfinite4(const uint2& v) { return nonfinite2(v.x) || nonfinite2(v.y); }
+__device__ __forceinline__ void unpack4(const uint2& v, float* x) {
+    x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
+    x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
 }
-__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
-    const unsigned w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-    unsigned w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-        w[i] = *reinterpret_cast<const unsigned*>(&p);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+__device__ __forceinline__ uint2 pack4(const float* x) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+    return make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b));
 }
 
-// grid (token tiles of `tok` rows, shares of a token's head rows)
-template <int LG>
-__global__ void __launch_bounds__(APP_THREADS)
-k_cache_append(const CacheView c, const Ragged r, const AppendJob j, int tok, unsigned* __restrict__ status) {
-    __shared__ TokInfo info[APP_TOK];
-    __shared__ int pos_q[APP_TOK], pos_k[APP_TOK];
-    __shared__ float2 ang[2][APP_TOK][MAX_HALF];     // (cos, sin) at the token's own position; at the kept row's
-    grid_dep_wait();
-    grid_dep_launch_next();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int i0 = blockIdx.x * tok;
-    const int n_tok = min(tok, r.N - i0);
-    if (warp < n_tok) {
-        const int i = i0 + warp, b = seq_of_row(r, i);
-        TokInfo t = {-1, 0, 0, 0};
-        int pq = 0, pk = 0;
-        if (b >= 0) {
-            int o;
-            const int n = seq_rows(r, b, o), old = seq_len(r, c, b), li = i - o;
-            const int p0 = j.pos0 != nullptr ? j.pos0[b] : old;
-            int kept = n, at = li;
-            if (j.rep_cnt != nullptr) {
-                kept = j.rep_cnt[b];
-                if (kept < 0 || kept > n) { t.bad |= ST_BAD_COUNT; kept = min(max(kept, 0), n); }
-                if (li < kept) {
-                    at = j.rep_idx[i];
-                    if (at < 0 || at >= n || (li > 0 && j.rep_idx[i - 1] >= at)) { t.bad |= ST_BAD_INDEX; kept = 0; }
-                }
-            }
-            pq = p0 + li;
-            if (li < kept) {
-                const int64_t slot = (int64_t)old + li;
-                pk = p0 + at;
-                t.src = o + at;
-                if (slot >= (int64_t)c.max_pages << c.shift) {
-                    t.bad |= ST_BAD_COUNT;
-                } else {
-                    const int page = c.table[(int64_t)b * c.table_ld + (slot >> c.shift)];
-                    if (page < 0 || page >= c.n_pages) t.bad |= ST_BAD_INDEX;
-                    else { t.page = page; t.slot = (int)slot & ((1 << c.shift) - 1); }
-                }
-            }
-        }
-        if (lane == 0) {
-            // row i's queries are its own; its keys come from row src (itself without a list)
-            info[warp] = t;
-            pos_q[warp] = b >= 0 ? pq : INT_MIN;
-            pos_k[warp] = pk;
-            if (t.bad != 0 && blockIdx.y == 0) atomicOr(status, (unsigned)t.bad);
-        }
-    }
-    __syncthreads();
-    const int half = j.inv_freq != nullptr ? j.rot >> 1 : 0;
-    const int sets = j.rep_idx != nullptr ? 2 : 1;
-    for (int q = threadIdx.x; q < sets * n_tok * half; q += APP_THREADS) {
-        const int i = q % half, t = q / half % n_tok, s = q / (half * n_tok);
-        const double turns = (double)(s == 0 ? pos_q[t] : pos_k[t]) * j.inv_freq[i] * 0.15915494309189533577;   // 1 / (2 pi)
-        float sn, cs;
-        sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
-        ang[s][t][i] = make_float2(cs, sn);
-    }
-    __syncthreads();
+// What a lane does to its eight elements of every row: elements at e0 .. e0 + 3 and e1 .. e1 + 3 of the head.
+struct Lane {
+    int e0, e1;
+    bool on, turns;                      // has elements; they are rotated
+};
 
-    const int nvec = c.d >> 3, hv = half >> 3, h_q = j.Q != nullptr ? j.h : 0;
-    const int per_tok = h_q + 2 * c.h_kv;
-    constexpr int GROUPS = APP_THREADS / LG;
-    const int group = threadIdx.x / LG, v = threadIdx.x % LG;
-    const bool on = v < nvec;
-    const int total = n_tok * per_tok;
-    bool bad = false;
-    for (int base = blockIdx.y * GROUPS + group; base < total; base += gridDim.y * GROUPS * APP_ROWS) {
-        uint4 in[APP_ROWS];
-        __nv_bfloat16* dst[APP_ROWS];
-        int kind[APP_ROWS], at[APP_ROWS];
+// cosines and sines of the lane's four pairs at position `pos`
+__device__ __forceinline__ void angles(const AppendJob& j, const Lane& ln, int v, int pos, float (&cs)[4], float (&sn)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        cs[i] = 1.f; sn[i] = 0.f;
+        if (ln.turns) {
+            const double turns = (double)pos * j.inv_freq[4 * v + i] * 0.15915494309189533577;   // 1 / (2 pi)
+            sincospif(2.0f * (float)(turns - rint(turns)), &sn[i], &cs[i]);
+        }
+    }
+}
+
+// Rows first, first + step, .. < count of one token, `src` to `dst`, head x at x * d (src) and x * dst_step (dst):
+// normed by the lane's weights w (NULL: not), rotated.
+template <int LG, bool PAIRS>
+__device__ __forceinline__ void move_rows(const __nv_bfloat16* src, __nv_bfloat16* dst, int64_t dst_step, int first, int step,
+                                          int count, int d, const Lane& ln, const __nv_bfloat16* w, float eps, bool rotate,
+                                          const float (&cs)[4], const float (&sn)[4], unsigned mask, bool& bad) {
+    float g[8];
+    if (w != nullptr) {
+        unpack4(ln.on ? *reinterpret_cast<const uint2*>(w + ln.e0) : make_uint2(0u, 0u), g);
+        unpack4(ln.on ? *reinterpret_cast<const uint2*>(w + ln.e1) : make_uint2(0u, 0u), g + 4);
+    }
+    for (int x0 = first; x0 < count; x0 += APP_ROWS * step) {
+        uint2 a[APP_ROWS], b[APP_ROWS];
 #pragma unroll
         for (int u = 0; u < APP_ROWS; ++u) {
-            const int row = base + u * gridDim.y * GROUPS;
-            in[u] = make_uint4(0u, 0u, 0u, 0u);
-            dst[u] = nullptr;
-            kind[u] = 3; at[u] = 0;
-            if (row < total) {
-                const int t = row / per_tok, x = row - t * per_tok;
-                at[u] = t;
-                const __nv_bfloat16* src = nullptr;
-                if (x < h_q) {
-                    kind[u] = 0;
-                    if (pos_q[t] != INT_MIN) {
-                        src = j.Q + (int64_t)(i0 + t) * j.ldq + (int64_t)x * c.d;
-                        dst[u] = j.q_out + (int64_t)(i0 + t) * j.ldqo + (int64_t)x * c.d;
-                    }
-                } else if (info[t].page >= 0) {
-                    const bool is_v = x - h_q >= c.h_kv;
-                    const int head = x - h_q - (is_v ? c.h_kv : 0);
-                    kind[u] = is_v ? 2 : 1;
-                    src = is_v ? j.V + (int64_t)info[t].src * j.ldv : j.K + (int64_t)info[t].src * j.ldk;
-                    src += (int64_t)head * c.d;
-                    dst[u] = (is_v ? c.v : c.k) + slot_at(c, info[t].page, head, info[t].slot);
-                }
-                if (on && src != nullptr) in[u] = *reinterpret_cast<const uint4*>(src + v * 8);
+            a[u] = b[u] = make_uint2(0u, 0u);
+            if (x0 + u * step < count && ln.on) {
+                const __nv_bfloat16* p = src + (x0 + u * step) * d;
+                a[u] = *reinterpret_cast<const uint2*>(p + ln.e0);
+                b[u] = *reinterpret_cast<const uint2*>(p + ln.e1);
             }
         }
 #pragma unroll
         for (int u = 0; u < APP_ROWS; ++u) {
-            bad = bad || nonfinite8(in[u]);
-            uint4 o = in[u];
-            const __nv_bfloat16* w = kind[u] == 0 ? j.q_norm : j.k_norm;
-            // (the branches are the same for all lanes of a group, not of a warp: the shuffles name the group's lanes)
-            const unsigned mask = LG == 16 ? 0xffffu << (threadIdx.x & 16) : 0xffu << (threadIdx.x & 24);
-            if (kind[u] < 2 && (w != nullptr || half != 0)) {
+            if (x0 + u * step >= count) break;                   // (the same for all lanes of the group)
+            bad = bad || nonfinite4(a[u]) || nonfinite4(b[u]);
+            if (w != nullptr || rotate) {
                 float x[8];
-                unpack8(in[u], x);
+                unpack4(a[u], x);
+                unpack4(b[u], x + 4);
                 if (w != nullptr) {
                     float s = 0.f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
 #pragma unroll
                     for (int m = LG / 2; m > 0; m >>= 1) s += __shfl_xor_sync(mask, s, m, LG);
-                    const float f = rsqrtf(s / (float)c.d + j.eps);
-                    float g[8];
-                    unpack8(on ? *reinterpret_cast<const uint4*>(w + v * 8) : make_uint4(0u, 0u, 0u, 0u), g);
+                    const float f = rsqrtf(s / (float)d + eps);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = x[e] * f * g[e];
+                    for (int e = 0; e < 8; ++e) x[e] *= f * g[e];
                 }
-                if (half != 0) {
-                    const float2* a = ang[kind[u] == 1 && sets == 2 ? 1 : 0][at[u]];
-                    if (j.pairs) {
-                        if (v * 8 < j.rot) {
 #pragma unroll
-                            for (int e = 0; e < 8; e += 2) {
-                                const float2 cs = a[v * 4 + (e >> 1)];
-                                const float p = x[e], q = x[e + 1];
-                                x[e] = p * cs.x - q * cs.y;
-                                x[e + 1] = q * cs.x + p * cs.y;
-                            }
-                        }
-                    } else {
-                        const bool low = v < hv, in_rot = v < 2 * hv;
-                        const int other = low ? v + hv : in_rot ? v - hv : v;
-                        float y[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) y[e] = __shfl_sync(mask, x[e], other, LG);
-                        if (in_rot) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const float2 cs = a[(low ? v : v - hv) * 8 + e];
-                                x[e] = low ? x[e] * cs.x - y[e] * cs.y : x[e] * cs.x + y[e] * cs.y;
-                            }
-                        }
-                    }
+                for (int i = 0; i < 4; ++i) {                    // (an unrotated lane has cosine 1, sine 0)
+                    const int p = PAIRS ? 2 * i : i, q = PAIRS ? 2 * i + 1 : 4 + i;
+                    const float y = x[p], z = x[q];
+                    x[p] = y * cs[i] - z * sn[i];
+                    x[q] = z * cs[i] + y * sn[i];
                 }
-                o = pack8(x);
+                a[u] = pack4(x);
+                b[u] = pack4(x + 4);
             }
-            if (on && dst[u] != nullptr) *reinterpret_cast<uint4*>(dst[u] + v * 8) = o;
+            if (ln.on) {
+                __nv_bfloat16* p = dst + (x0 + u * step) * dst_step;
+                *reinterpret_cast<uint2*>(p + ln.e0) = a[u];
+                *reinterpret_cast<uint2*>(p + ln.e1) = b[u];
+            }
         }
     }
-    if (bad) atomicOr(status, ST_NONFINITE);
-    if (blockIdx.x == 0 && blockIdx.y == 0) {
+}
+
+// A warp: one token, or one of `shares` parts of its heads.  LG lanes have a head's row.
+template <int LG, bool PAIRS>
+__global__ void __launch_bounds__(APP_THREADS)
+k_cache_append(const CacheView c, const Ragged r, const AppendJob j, int shares, unsigned* __restrict__ status) {
+    grid_dep_wait();
+    grid_dep_launch_next();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int item = blockIdx.x * APP_WARPS + warp;
+    const int i = item / shares, share = item - i * shares;
+    if (blockIdx.x == 0) {
         check_ragged(r, c, status, threadIdx.x, APP_THREADS);
         if (j.len_out != nullptr)
             for (int b = threadIdx.x; b < r.B; b += APP_THREADS) {
@@ -216,6 +131,61 @@ k_cache_append(const CacheView c, const Ragged r, const AppendJob j, int tok, un
                 j.len_out[b] = (int)min((int64_t)seq_len(r, c, b) + n, (int64_t)c.max_pages << c.shift);
             }
     }
+    if (i >= r.N) return;
+    const int b = seq_of_row(r, i);
+    if (b < 0) return;
+    int o;
+    const int n = seq_rows(r, b, o), old = seq_len(r, c, b), li = i - o;
+    const int p0 = j.pos0 != nullptr ? j.pos0[b] : old;
+    // row i's queries are its own; the keys and values that go to slot old + li are those of token `at`
+    unsigned faults = 0u;
+    int kept = n, at = li, page = -1, slot = 0;
+    if (j.rep_cnt != nullptr) {
+        kept = j.rep_cnt[b];
+        if (kept < 0 || kept > n) { faults |= ST_BAD_COUNT; kept = min(max(kept, 0), n); }
+        if (li < kept) {
+            at = j.rep_idx[i];
+            if (at < 0 || at >= n || (li > 0 && j.rep_idx[i - 1] >= at)) { faults |= ST_BAD_INDEX; kept = 0; }
+        }
+    }
+    if (li < kept) {
+        const int64_t s = (int64_t)old + li;
+        if (s >= (int64_t)c.max_pages << c.shift) {
+            faults |= ST_BAD_COUNT;
+        } else {
+            page = c.table[(int64_t)b * c.table_ld + (s >> c.shift)];
+            if (page < 0 || page >= c.n_pages) { faults |= ST_BAD_INDEX; page = -1; }
+            slot = (int)s & ((1 << c.shift) - 1);
+        }
+    }
+    if (faults != 0u && lane == 0) atomicOr(status, faults);
+
+    constexpr int PER = 32 / LG;                                 // rows of a warp at a time
+    const int v = lane % LG, first = share * PER + lane / LG, step = shares * PER;
+    const unsigned mask = LG == 16 ? 0xffffu << (lane & 16) : 0xffu << (lane & 24);
+    const bool rotate = j.inv_freq != nullptr;
+    // lanes below rot / 8 have four pairs each; the elements behind `rot` are the other lanes', eight in a row
+    const int nvec = c.d >> 3, nrot = rotate ? j.rot >> 3 : 0;
+    Lane ln;
+    ln.on = v < nvec;
+    ln.turns = v < nrot;
+    ln.e0 = !PAIRS && ln.turns ? 4 * v : 8 * v;
+    ln.e1 = !PAIRS && ln.turns ? 4 * v + (j.rot >> 1) : 8 * v + 4;
+    float cs[4], sn[4];
+    angles(j, ln, v, p0 + li, cs, sn);
+    bool bad = false;
+    if (j.Q != nullptr)
+        move_rows<LG, PAIRS>(j.Q + (int64_t)i * j.ldq, j.q_out + (int64_t)i * j.ldqo, c.d, first, step, j.h, c.d, ln, j.q_norm,
+                             j.eps, rotate, cs, sn, mask, bad);
+    if (page >= 0) {
+        const int64_t at0 = slot_at(c, page, 0, slot), head_step = (int64_t)c.d << c.shift;
+        if (at != li) angles(j, ln, v, p0 + at, cs, sn);
+        move_rows<LG, PAIRS>(j.K + (int64_t)(o + at) * j.ldk, c.k + at0, head_step, first, step, c.h_kv, c.d, ln, j.k_norm, j.eps,
+                             rotate, cs, sn, mask, bad);
+        move_rows<LG, PAIRS>(j.V + (int64_t)(o + at) * j.ldv, c.v + at0, head_step, first, step, c.h_kv, c.d, ln, nullptr, 0.f,
+                             false, cs, sn, mask, bad);
+    }
+    if (bad) atomicOr(status, ST_NONFINITE);
 }
 
 // Elementwise minimum and maximum of a page's keys, over the slots below the sequence's new length, from the page
@@ -268,7 +238,7 @@ k_cache_bounds(const CacheView c, const Ragged r, const int32_t* __restrict__ re
     };
     if (v < nvec) {
         const __nv_bfloat16* src = c.k + slot_at(c, page, head, 0) + v * 8;
-#pragma unroll 4
+#pragma unroll 8
         for (int s = row; s < live; s += rows) {
             const uint4 x = *reinterpret_cast<const uint4*>(src + (int64_t)s * c.d);
             take(lo, hi, x, x);
@@ -288,19 +258,16 @@ k_cache_bounds(const CacheView c, const Ragged r, const int32_t* __restrict__ re
 }  // namespace
 
 cudaError_t launch_cache_append(ada_ctx* ctx, const CacheView& c, const Ragged& r, const AppendJob& j, cudaStream_t s) {
-    const int lg = c.d <= 64 ? 8 : 16, groups = APP_THREADS / lg;
-    const int per_tok = (j.Q != nullptr ? j.h : 0) + 2 * c.h_kv;
-    // one token per block, its rows spread over as many blocks as are needed for one round each, while the tokens
-    // alone do not fill the GPU; else several tokens per block
-    const int tok = r.N >= 8 * ctx->sm_count ? APP_TOK : 1;
-    const int tiles = (r.N + tok - 1) / tok;
-    int shares = 1;
-    if (tok == 1) {
-        const int want = (per_tok + groups - 1) / groups, room = (4 * ctx->sm_count + tiles - 1) / tiles;
-        shares = want < room ? want : room;
-    }
-    auto kernel = lg == 8 ? k_cache_append<8> : k_cache_append<16>;
-    cudaError_t e = launch_k(ctx, kernel, dim3(tiles, shares), dim3(APP_THREADS), 0, s, c, r, j, tok, ctx->status);
+    // a token's heads are dealt to several warps while the tokens alone do not fill the GPU: as many as leave a warp
+    // one round of rows of the larger of queries and keys
+    const int per = c.d <= 64 ? 4 : 2, heads = j.h > c.h_kv ? j.h : c.h_kv;
+    const int want = (heads + per * APP_ROWS - 1) / (per * APP_ROWS), room = 16 * ctx->sm_count / r.N;
+    const int shares = room < 1 ? 1 : want < room ? want : room;
+    const int64_t items = (int64_t)r.N * shares;
+    auto kernel = c.d <= 64 ? (j.pairs ? k_cache_append<8, true> : k_cache_append<8, false>)
+                            : (j.pairs ? k_cache_append<16, true> : k_cache_append<16, false>);
+    cudaError_t e = launch_k(ctx, kernel, dim3((unsigned)((items + APP_WARPS - 1) / APP_WARPS)), dim3(APP_THREADS), 0, s, c, r, j,
+                             shares, ctx->status);
     if (e != cudaSuccess) return e;
     if (c.kmin != nullptr) {
         // a sequence of n new tokens writes to at most n and at most (n - 1) / ps + 2 pages

@@ -1,18 +1,20 @@
 // Attention of single tokens over the paged cache (ada_attention_cached with few rows per key head), and of any tokens
 // over the pages that their lists name (ada_attention_blocks).
 //
-//   out = sum_s 2^(sc q.k_s - m) v_s / sum_s 2^(sc q.k_s - m),   sc = scale log2(e), m the running maximum
+//   out = sum_s 2^(sc q.k_s - m) v_s / sum_s 2^(sc q.k_s - m),   sc = scale log2(e), m a reference near the maximum
 // in one pass over the keys.  The heads that share a key head (and, dense, the few new tokens of a sequence) are the
 // up to 16 rows of one tile, so that K and V are read once for all of them.  What bounds it is the stream of keys and
 // values: from HBM in a decoding step, from L2 where a chunk's tokens list the same pages.  A 128-row tcgen05 tile would be
-// empty but for these rows; mma.sync takes 16 rows and leaves its operands in registers, so that nothing but the
-// keys and values passes through shared memory.
+// empty but for these rows.  Here both products are taken transposed on mma.sync, S^T = K Q^T and O^T = V^T P^T: keys
+// (head elements) are the 16-row side of the instruction and the rows its 8-column side, so that 8 rows waste nothing,
+// and operands stay in registers but for K and V.
 //
-// A warp works alone: 32 keys at a time arrive by TMA in a ring of its own, scores, softmax and products stay in
-// its registers, and it shares nothing until the end of a row.  Four warps of a CTA deal a row's granules of 32 keys
-// among them (TEAM = 4) or take rows of their own (TEAM = 1, many rows with lists: no barrier at all).
+// A warp works alone: granules of 32 keys arrive by TMA, K and V in turn, in a ring of its own; scores, softmax and
+// products stay in its registers, and it shares nothing until the end of a row tile.  The eight warps of a CTA deal a
+// row tile's granules among them (TEAM = 8) or take row tiles of their own (TEAM = 1, many rows with lists: no barrier).
+// m is raised only when a score has left it by more than 8 powers of two: a vote per granule instead of a maximum.
 //
-// Dense work is cut into units of 128 keys of one (sequence, key head); every CTA takes an equal run of units
+// Dense work is cut into units of 256 keys of one (sequence, key head); every CTA takes an equal run of units
 // whatever the lengths are, and a row tile that several CTAs share is joined by the one that finishes last (in
 // the order of the keys, so that results do not depend on who that is).  Nobody waits for another CTA.
 #include "cache_tma.cuh"
@@ -23,26 +25,29 @@ using namespace tc;
 
 namespace {
 
-constexpr int ST_WARPS = 4;
+constexpr int ST_WARPS = 8;
 constexpr int ST_THREADS = 32 * ST_WARPS;
 constexpr int GK = 32;                     // keys per granule
-constexpr int GPU_ = 4;                    // granules per unit of dense work
+constexpr int UNIT = GK * ST_WARPS;        // keys per unit of dense work
 constexpr int NOWHERE = 0x7fff0000;        // position of keys that are not there: behind every limit
 constexpr int SLOT_FLOATS = 16 * 128 + 32; // one partial result: 16 rows x 128, maxima, sums
+constexpr float ST_LAG = 8.0f;
 
-template <int NDB> __host__ __device__ constexpr int st_stages() { return 6 / NDB; }
-template <int NDB> __host__ __device__ constexpr int st_stage_bytes() { return 2 * NDB * GK * 128; }
-template <int NDB> __host__ __device__ constexpr int st_ring_bytes() { return ST_WARPS * st_stages<NDB>() * st_stage_bytes<NDB>(); }
+// slots of a warp's ring: K or V of a granule, NDB blocks of 64 elements x 32 keys
+template <int NDB> __host__ __device__ constexpr int st_slots() { return 6 / NDB; }
+template <int NDB> __host__ __device__ constexpr int st_slot_bytes() { return NDB * GK * 128; }
+template <int NDB> __host__ __device__ constexpr int st_ring_bytes() { return ST_WARPS * st_slots<NDB>() * st_slot_bytes<NDB>(); }
+template <int NDB> __host__ __device__ constexpr int st_merge_bytes() { return ST_WARPS * 8 * NDB * 64 * 4; }
 
 struct StepShared {
     unsigned long long full[ST_WARPS][6];
-    int2 base[ST_WARPS][6];                // positions of the two halves of a stage
+    int2 base[ST_WARPS][6];                // positions of the two halves of a granule
     float m[ST_WARPS][16], l[ST_WARPS][16];
     int abort_flag[2];
     int last;
 };
 template <int NDB> __host__ __device__ constexpr int st_smem() {
-    return st_ring_bytes<NDB>() + ST_WARPS * 16 * NDB * 64 * 4 + (int)sizeof(StepShared);
+    return st_ring_bytes<NDB>() + st_merge_bytes<NDB>() + (int)sizeof(StepShared);
 }
 static_assert(st_smem<2>() <= 227 * 1024 && st_smem<1>() <= 227 * 1024, "shared memory budget");
 
@@ -50,7 +55,7 @@ struct StepMaps {
     CUtensorMap k, v;
 };
 
-// One row tile's run of keys, as a CTA (TEAM = 4) or a warp (TEAM = 1) works on it.
+// One row tile's run of keys, as a team works on it.
 struct Seg {
     int b, head, row, g0;                  // sequence, key head, first token's row, first of the group's heads
     int rows, n, len;                      // rows of the tile; the sequence's new tokens and its length
@@ -62,47 +67,46 @@ struct Seg {
 
 template <bool LIST>
 struct Work {                              // where a team is in its run of work; the same in all of its lanes
-    // dense: units; lists: items
-    int64_t at, end;
-    // dense
-    int b, head, ku, nu, n, off, len;
+    int64_t at, end;                       // dense: units; lists: (row, key head, row tile, piece) items
+    int b, head, n, off, len;
+    int ku, nu;                            // dense: unit within the row tile, of how many
     int64_t per;
+    int row, rt, piece;                    // lists
 
     __device__ __forceinline__ void load_seq(const Ragged& r, const CacheView& c) {
         n = seq_rows(r, b, off);
         len = seq_len(r, c, b);
-        nu = n > 0 ? max(1, (len + GK * GPU_ - 1) / (GK * GPU_)) : 0;
+        nu = n > 0 ? max(1, (len + UNIT - 1) / UNIT) : 0;
     }
     // the next segment, or false
     __device__ __forceinline__ bool next(Seg& s, const Ragged& r, const CacheView& c, const AttendJob& j, int G, int tiles,
                                          int pieces, unsigned* status) {
         if (LIST) {
             while (at < end) {
-                const int64_t item = at++;
-                const int piece = (int)(item % pieces);
-                const int64_t rest = item / pieces;
-                const int rt = (int)(rest % tiles);
-                const int64_t rh = rest / tiles;
-                const int row = (int)(rh / c.h_kv), head = (int)(rh % c.h_kv);
-                if (row != off || b < 0) { b = seq_of_row(r, row); off = row; }
-                if (b < 0) { b = -1; off = -1; continue; }
-                int o;
+                if (b < 0 || row < off || row >= off + n) {     // another sequence
+                    b = seq_of_row(r, row);
+                    if (b < 0) { at = end; return false; }      // (rows of no sequence come last)
+                    load_seq(r, c);
+                }
                 s.b = b; s.head = head; s.row = row; s.g0 = rt * 16;
                 s.rows = min(16, G - rt * 16);
-                s.n = seq_rows(r, b, o);
-                s.len = seq_len(r, c, b);
-                // the row's own limit, as if it were the only new token
-                s.len = j.causal ? max(s.len - s.n + (row - o) + 1, 0) : s.len;
+                s.len = j.causal ? max(len - n + (row - off) + 1, 0) : len;   // as if it were the only new token
                 s.n = 1;
+                const int64_t rh = (int64_t)row * c.h_kv + head;
                 int cnt = j.blk_cnt[rh];
                 if (cnt < 0 || cnt > j.k) { atomicOr(status, ST_BAD_COUNT); cnt = min(max(cnt, 0), j.k); }
                 s.cnt = cnt;
                 const int g = (int)((((int64_t)cnt << c.shift) + GK - 1) / GK);
-                s.g_begin = (int)((int64_t)g * piece / pieces);
-                s.g_end = (int)((int64_t)g * (piece + 1) / pieces);
+                s.g_begin = pieces == 1 ? 0 : (int)((int64_t)g * piece / pieces);
+                s.g_end = pieces == 1 ? g : (int)((int64_t)g * (piece + 1) / pieces);
                 s.pieces = pieces; s.piece = piece;
-                s.slot0 = (int)(rest * pieces);
-                s.ctr = (int)rest;
+                s.ctr = pieces == 1 ? 0 : (int)(rh * tiles + rt);
+                s.slot0 = s.ctr * pieces;
+                ++at;
+                if (++piece == pieces) {
+                    piece = 0;
+                    if (++rt == tiles) { rt = 0; if (++head == c.h_kv) { head = 0; ++row; } }
+                }
                 return true;
             }
             return false;
@@ -121,14 +125,18 @@ struct Work {                              // where a team is in its run of work
         s.n = n; s.len = len; s.cnt = 0;
         s.rows = min(n, j.max_new) * G;
         const int g = (len + GK - 1) / GK;
-        s.g_begin = ku * GPU_;
-        s.g_end = min((ku + take) * GPU_, g);
+        s.g_begin = ku * ST_WARPS;
+        s.g_end = min((ku + take) * ST_WARPS, g);
         const int64_t first = at - ku;                      // the row tile's units are [first, first + nu)
-        const int c0 = (int)(first / per), c1 = (int)((first + nu - 1) / per);
-        s.pieces = c1 - c0 + 1;
-        s.piece = (int)(at / per) - c0;
-        s.slot0 = c0;
-        s.ctr = c1;
+        if (take == nu) {
+            s.pieces = 1; s.piece = s.slot0 = s.ctr = 0;
+        } else {
+            const int c0 = (int)(first / per), c1 = (int)((first + nu - 1) / per);
+            s.pieces = c1 - c0 + 1;
+            s.piece = (int)(at / per) - c0;
+            s.slot0 = c0;
+            s.ctr = c1;
+        }
         at += take; ku += take;
         return true;
     }
@@ -142,20 +150,21 @@ __device__ __forceinline__ float* partial(float* ws, const Seg& s, int piece) {
     return ws + slot * SLOT_FLOATS;
 }
 
-template <int NDB, bool LIST, int TEAM>
+// NT: rows / 8
+template <int NDB, int NT, bool LIST, int TEAM>
 __global__ void __launch_bounds__(ST_THREADS, 1)
 k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Ragged r, const AttendJob j, int tiles,
              int pieces, float* __restrict__ ws, unsigned* __restrict__ counters, unsigned* __restrict__ status) {
-    constexpr int NST = st_stages<NDB>();
+    constexpr int SLOTS = st_slots<NDB>();
     constexpr int KS = NDB * 4;                       // 16-element steps of a head row
-    constexpr int HALF_TILE = GK * 128;               // one 64-element block of 32 keys: 4 KiB
+    constexpr int BLOCK = GK * 128;                   // one 64-element block of 32 keys: 4 KiB
     extern __shared__ __align__(1024) unsigned char smem[];
-    float* mrg = reinterpret_cast<float*>(smem + st_ring_bytes<NDB>());            // [4][16][NDB * 64]
-    StepShared& sh = *reinterpret_cast<StepShared*>(smem + st_ring_bytes<NDB>() + ST_WARPS * 16 * NDB * 64 * 4);
+    float* mrg = reinterpret_cast<float*>(smem + st_ring_bytes<NDB>());            // [8 warps][8 rows][NDB * 64]
+    StepShared& sh = *reinterpret_cast<StepShared*>(smem + st_ring_bytes<NDB>() + st_merge_bytes<NDB>());
     volatile int* abort_flag = sh.abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = j.h / c.h_kv;
-    unsigned char* ring = smem + warp * NST * st_stage_bytes<NDB>();
+    unsigned char* ring = smem + warp * SLOTS * st_slot_bytes<NDB>();
     if ((smem_u32(smem) & 1023u) != 0u) {             // the tiles would not be where the swizzle assumes
         grid_dep_wait();
         if (tid == 0) { atomicOr(status, ST_TIMEOUT); status[2] = 399u; }
@@ -166,7 +175,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
         sh.abort_flag[1] = wait_limit_units(false);
     }
     if (lane == 0) {
-        for (int i = 0; i < NST; ++i) mbar_init(&sh.full[warp][i], 1);
+        for (int i = 0; i < SLOTS; ++i) mbar_init(&sh.full[warp][i], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -179,15 +188,20 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
     // ---------------------------------------------------------------- this team's run of work
     const int w = TEAM == 1 ? 0 : warp;
     Work<LIST> work;
+    work.b = LIST ? -1 : 0;
+    work.head = work.n = work.off = work.len = work.ku = work.nu = work.row = work.rt = work.piece = 0;
     if (LIST) {
         const int64_t items = (int64_t)r.N * c.h_kv * tiles * pieces;
         const int64_t teams = (int64_t)gridDim.x * (ST_WARPS / TEAM);
         const int64_t team = (int64_t)blockIdx.x * (ST_WARPS / TEAM) + (TEAM == 1 ? warp : 0);
-        const int64_t per = (items + teams - 1) / teams;
-        work.at = min(team * per, items);
-        work.end = min(work.at + per, items);
-        work.b = -1; work.off = -1;
-        work.head = work.ku = work.nu = work.n = work.len = 0; work.per = 1;
+        work.per = (items + teams - 1) / teams;
+        work.at = min(team * work.per, items);
+        work.end = min(work.at + work.per, items);
+        int64_t rest = work.at / pieces;
+        work.piece = (int)(work.at - rest * pieces);
+        work.rt = (int)(rest % tiles); rest /= tiles;
+        work.head = (int)(rest % c.h_kv);
+        work.row = (int)(rest / c.h_kv);
     } else {
         // prefix sums of the sequences' units, 32 at a time, by every warp for itself
         auto units_of = [&](int b) {
@@ -195,7 +209,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
             int o;
             const int n = seq_rows(r, b, o);
             if (blockIdx.x == 0 && n > j.max_new) atomicOr(status, ST_BAD_COUNT);
-            return n > 0 ? max(1, (seq_len(r, c, b) + GK * GPU_ - 1) / (GK * GPU_)) : 0;
+            return n > 0 ? max(1, (seq_len(r, c, b) + UNIT - 1) / UNIT) : 0;
         };
         int64_t U = 0;
         for (int b0 = 0; b0 < r.B; b0 += 32) U += __reduce_add_sync(0xffffffffu, units_of(b0 + lane));
@@ -203,7 +217,6 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
         work.per = max((U + gridDim.x - 1) / gridDim.x, (int64_t)1);
         work.at = min(work.per * blockIdx.x, U);
         work.end = min(work.at + work.per, U);
-        work.b = 0; work.head = 0; work.ku = 0; work.nu = 0; work.n = 0; work.off = 0; work.len = 0;
         int64_t before = 0;
         if (work.at < work.end)
             for (int b0 = 0; b0 < r.B; b0 += 32) {
@@ -237,270 +250,312 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
     int pg = ps.g_begin + w;                          // the next granule to fetch
     int batch = -1;                                   // granule of lane 0's page, -1: none fetched for this segment
     int2 pid = make_int2(-1, -1), pbase = make_int2(NOWHERE, NOWHERE);
-    unsigned made = 0;
-    // fetches the next granule of this warp into the ring, if there is one
+    unsigned made = 0;                                // slots asked for: K, V, K, V ..
+    int id0 = -1, id1 = -1, first_slot = 0, phead = 0;   // pages of the granule whose K was asked for last
+    // asks for K or V of the next granule of this warp, if there is one
     auto produce = [&]() {
-        while (more && pg >= ps.g_end) {
-            more = pwork.next(ps, r, c, j, G, tiles, pieces, status);
-            pg = ps.g_begin + w;
-            batch = -1;
-        }
-        if (!more) return;
-        if (batch < 0 || pg >= batch + 32 * TEAM) {
-            // lane l: pages of this warp's l-th granule from here on
-            batch = pg;
-            const int g = pg + lane * TEAM;
-            int id[2] = {-1, -1}, base[2] = {NOWHERE, NOWHERE};
-            if (g < ps.g_end) {
+        if ((made & 1u) == 0u) {
+            while (more && pg >= ps.g_end) {
+                more = pwork.next(ps, r, c, j, G, tiles, pieces, status);
+                pg = ps.g_begin + w;
+                batch = -1;
+            }
+            if (!more) return;
+            if (batch < 0 || pg >= batch + 32 * TEAM) {
+                // lane l: pages of this warp's l-th granule from here on
+                batch = pg;
+                const int g = pg + lane * TEAM;
+                int id[2] = {-1, -1}, base[2] = {NOWHERE, NOWHERE};
+                if (g < ps.g_end) {
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int vk = g * GK + q * 16, e = vk >> c.shift, slot = vk & ((1 << c.shift) - 1);
-                    if (q == 1 && c.shift > 4) {
-                        id[1] = id[0];
-                        base[1] = id[0] >= 0 ? base[0] + 16 : NOWHERE;
-                        break;
-                    }
-                    int p = e;                        // dense: the sequence's e-th page
-                    bool ok = true;
-                    if (LIST) {
-                        ok = e < ps.cnt;
-                        if (ok) {
-                            const int32_t* list = j.blk_idx + ((int64_t)ps.row * c.h_kv + ps.head) * j.k;
-                            p = list[e];
-                            // an entry that does not ascend, or names a page that the table has no place for
-                            if (p < 0 || p >= c.max_pages || (e > 0 && list[e - 1] >= p)) {
-                                atomicOr(status, ST_BAD_INDEX);
-                                ok = false;
+                    for (int q = 0; q < 2; ++q) {
+                        const int vk = g * GK + q * 16, e = vk >> c.shift, slot = vk & ((1 << c.shift) - 1);
+                        if (q == 1 && c.shift > 4) {
+                            id[1] = id[0];
+                            base[1] = id[0] >= 0 ? base[0] + 16 : NOWHERE;
+                            break;
+                        }
+                        int p = e;                    // dense: the sequence's e-th page
+                        bool ok = true;
+                        if (LIST) {
+                            ok = e < ps.cnt;
+                            if (ok) {
+                                const int32_t* list = j.blk_idx + ((int64_t)ps.row * c.h_kv + ps.head) * j.k;
+                                p = list[e];
+                                // an entry that does not ascend, or names a page that the table has no place for
+                                if (p < 0 || p >= c.max_pages || (e > 0 && list[e - 1] >= p)) {
+                                    atomicOr(status, ST_BAD_INDEX);
+                                    ok = false;
+                                }
                             }
                         }
-                    }
-                    if (ok && (p << c.shift) < ps.len) {     // (pages behind the limit are not looked at)
-                        id[q] = page_of(c, ps.b, p, status);
-                        if (id[q] >= 0) base[q] = (p << c.shift) + slot;
+                        if (ok && (p << c.shift) < ps.len) {     // (pages behind the limit are not looked at)
+                            id[q] = page_of(c, ps.b, p, status);
+                            if (id[q] >= 0) base[q] = (p << c.shift) + slot;
+                        }
                     }
                 }
+                pid = make_int2(id[0], id[1]);
+                pbase = make_int2(base[0], base[1]);
             }
-            pid = make_int2(id[0], id[1]);
-            pbase = make_int2(base[0], base[1]);
+            const int l = (pg - batch) / TEAM;
+            id0 = __shfl_sync(0xffffffffu, pid.x, l); id1 = __shfl_sync(0xffffffffu, pid.y, l);
+            const int b0 = __shfl_sync(0xffffffffu, pbase.x, l), b1 = __shfl_sync(0xffffffffu, pbase.y, l);
+            if (lane == 0) sh.base[warp][made % SLOTS] = make_int2(b0, b1);
+            first_slot = (pg * GK) & ((1 << c.shift) - 1);
+            phead = ps.head;
+            pg += TEAM;
         }
-        const int l = (pg - batch) / TEAM;
-        const int id0 = __shfl_sync(0xffffffffu, pid.x, l), id1 = __shfl_sync(0xffffffffu, pid.y, l);
-        const int b0 = __shfl_sync(0xffffffffu, pbase.x, l), b1 = __shfl_sync(0xffffffffu, pbase.y, l);
         if (lane == 0) {
-            const int st = made % NST;
-            unsigned char* dst = ring + st * st_stage_bytes<NDB>();
+            const int st = made % SLOTS;
+            unsigned char* dst = ring + st * st_slot_bytes<NDB>();
             unsigned long long* bar = &sh.full[warp][st];
-            sh.base[warp][st] = make_int2(b0, b1);
+            const CUtensorMap* map = (made & 1u) ? &maps.v : &maps.k;
             if (c.shift > 4) {
-                const int slot = (pg * GK) & ((1 << c.shift) - 1);
-                mbar_expect_tx(bar, id0 >= 0 ? (unsigned)st_stage_bytes<NDB>() : 0u);
+                mbar_expect_tx(bar, id0 >= 0 ? (unsigned)st_slot_bytes<NDB>() : 0u);
                 if (id0 >= 0)
 #pragma unroll
-                    for (int db = 0; db < NDB; ++db) {
-                        tma_load_4d(&maps.k, bar, dst + db * HALF_TILE, db * BK, slot, ps.head, id0);
-                        tma_load_4d(&maps.v, bar, dst + (NDB + db) * HALF_TILE, db * BK, slot, ps.head, id0);
-                    }
+                    for (int db = 0; db < NDB; ++db) tma_load_4d(map, bar, dst + db * BLOCK, db * BK, first_slot, phead, id0);
             } else {
-                mbar_expect_tx(bar, (unsigned)st_stage_bytes<NDB>() / 2 * ((id0 >= 0) + (id1 >= 0)));
+                mbar_expect_tx(bar, (unsigned)st_slot_bytes<NDB>() / 2 * ((id0 >= 0) + (id1 >= 0)));
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     const int id = q == 0 ? id0 : id1;
                     if (id >= 0)
 #pragma unroll
-                        for (int db = 0; db < NDB; ++db) {
-                            tma_load_4d(&maps.k, bar, dst + db * HALF_TILE + q * 2048, db * BK, 0, ps.head, id);
-                            tma_load_4d(&maps.v, bar, dst + (NDB + db) * HALF_TILE + q * 2048, db * BK, 0, ps.head, id);
-                        }
+                        for (int db = 0; db < NDB; ++db) tma_load_4d(map, bar, dst + db * BLOCK + q * 2048, db * BK, 0, phead, id);
                 }
             }
         }
         ++made;
-        pg += TEAM;
     };
 #pragma unroll 1
-    for (int i = 0; i < NST; ++i) produce();
+    for (int i = 0; i < SLOTS; ++i) produce();
 
     // ---------------------------------------------------------------- consumer side
-    const int r0 = lane >> 2, c0 = 2 * (lane & 3);
+    const int r0 = lane >> 2, c0 = 2 * (lane & 3);    // a fragment's row; the first of its two columns
     const unsigned ring_u = smem_u32(ring);
+    // addresses of the two operands within a slot: lane l names row l % 8 of the 8 x 8 matrix l / 8
+    const int k_key = ((lane >> 3) & 1) * 8 + (lane & 7), k_ch = lane >> 4;
+    const int v_key = (lane >> 4) * 8 + (lane & 7), v_ch = (lane >> 3) & 1;
     unsigned used = 0;
     bool ok = true;
+    auto wait_slot = [&](int where) {
+        if (ok) ok = mbar_wait(&sh.full[warp][used % SLOTS], (used / SLOTS) & 1u, abort_flag, where);
+        ok = __all_sync(0xffffffffu, ok);
+    };
+    auto release = [&]() {
+        __syncwarp();                                 // all lanes have read the slot
+        if (ok) { ++used; produce(); }
+    };
     Seg s;
     while (work.next(s, r, c, j, G, tiles, pieces, status)) {
-        // A operand: rows r0 and r0 + 8 of the tile (row = token * G + head of the group)
-        unsigned qf[KS][4];
-        int lim[2];
+        // right operand of S^T: row r0 (+ 8) of the tile (row = token * G + head of the group)
+        unsigned qf[NT][KS][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = r0 + 8 * i;
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = nt * 8 + r0;
             const bool live = row < s.rows;
             const int t = LIST || !live ? 0 : row / G, g = s.g0 + (LIST ? row : row - t * G);
-            lim[i] = !live ? 0 : LIST ? s.len : j.causal ? s.len - s.n + t + 1 : s.len;
             const __nv_bfloat16* q = j.Q + (int64_t)(s.row + t) * j.ldq + ((int64_t)s.head * G + g) * c.d;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                qf[k][i] = live && k * 16 < c.d ? *reinterpret_cast<const unsigned*>(q + k * 16 + c0) : 0u;
-                qf[k][2 + i] = live && k * 16 < c.d ? *reinterpret_cast<const unsigned*>(q + k * 16 + 8 + c0) : 0u;
+                qf[nt][k][0] = live && k * 16 < c.d ? *reinterpret_cast<const unsigned*>(q + k * 16 + c0) : 0u;
+                qf[nt][k][1] = live && k * 16 < c.d ? *reinterpret_cast<const unsigned*>(q + k * 16 + 8 + c0) : 0u;
             }
         }
+        // of this lane's rows nt * 8 + c0 + {0, 1}: keys that they see, reference, sum of this lane's probabilities
+        int lim[NT][2];
+        float m[NT][2], l[NT][2], o[KS][NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = nt * 8 + c0 + i;
+                lim[nt][i] = row >= s.rows ? 0 : LIST || !j.causal ? s.len : s.len - s.n + row / G + 1;
+                m[nt][i] = -INFINITY;
+                l[nt][i] = 0.f;
+            }
         // keys from here on are masked for some row: the first token's limit
         const int lim_all = LIST || !j.causal ? s.len : s.len - s.n + 1;
-        float o[NDB * 8][4];
 #pragma unroll
-        for (int n = 0; n < NDB * 8; ++n)
+        for (int d = 0; d < KS; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][nt][e] = 0.f;
 
         for (int g = s.g_begin + w; g < s.g_end; g += TEAM) {
-            const int st = used % NST;
-            if (ok) ok = mbar_wait(&sh.full[warp][st], (used / NST) & 1u, abort_flag, 50);
-            ok = __all_sync(0xffffffffu, ok);
+            float sc[2][NT][4];                        // scores of 32 keys (two tiles of 16) x rows
+            int2 base = make_int2(0, 0);
+            wait_slot(50);
             if (ok) {
-                const unsigned kt = ring_u + st * st_stage_bytes<NDB>(), vt = kt + NDB * HALF_TILE;
-                const int2 base = sh.base[warp][st];
-                // ---- scores: 16 rows x 32 keys
-                float sc[4][4];
+                const int st = used % SLOTS;
+                const unsigned kt = ring_u + st * st_slot_bytes<NDB>();
+                base = sh.base[warp][st];
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
+                for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[mt][nt][e] = 0.f;
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int np = 0; np < 2; ++np) {
-                        const int key = np * 16 + ((lane >> 4) << 3) + (lane & 7), ch = (k & 3) * 2 + ((lane >> 3) & 1);
-                        unsigned bf[4];
-                        ldsm4(kt + (k >> 2) * HALF_TILE + key * 128 + ((ch ^ (key & 7)) << 4), bf);
-                        mma16816(sc[2 * np], qf[k], bf[0], bf[1]);
-                        mma16816(sc[2 * np + 1], qf[k], bf[2], bf[3]);
+                    for (int mt = 0; mt < 2; ++mt) {
+                        unsigned a[4];
+                        ldsm4(kt + (k >> 2) * BLOCK + (mt * 16 + k_key) * 128 + ((((k & 3) * 2 + k_ch) ^ (k_key & 7)) << 4), a);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma16816(sc[mt][nt], a, qf[nt][k][0], qf[nt][k][1]);
                     }
-                // ---- mask; values of slots that hold nothing of this sequence must not meet a zero probability as NaN
-                if (base.x + 15 >= lim_all || base.y + 15 >= lim_all) {
+            }
+            release();
+            if (ok && (base.x + 15 >= lim_all || base.y + 15 >= lim_all)) {
 #pragma unroll
-                    for (int n = 0; n < 4; ++n)
+                for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int pos = (n < 2 ? base.x : base.y) + (n & 1) * 8 + c0 + (e & 1);
-                            if (pos >= lim[e >> 1]) sc[n][e] = -INFINITY;
-                        }
-                    if (base.x + 15 >= s.len || base.y + 15 >= s.len) {
-                        unsigned char* v = ring + st * st_stage_bytes<NDB>() + NDB * HALF_TILE;
-                        for (int q = lane; q < GK * NDB * 8; q += 32) {
-                            const int key = (q >> 3) & 31, db = q >> 8;
-                            if ((key < 16 ? base.x + key : base.y + key - 16) >= s.len)
-                                *reinterpret_cast<uint4*>(v + db * HALF_TILE + key * 128 + (q & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                        }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the slot's next load comes through the async proxy)
-                        __syncwarp();
-                    }
-                }
-                // ---- running maximum and sum
-                float mr[2];
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float x = -INFINITY;
+                        for (int e = 0; e < 4; ++e)
+                            if ((mt == 0 ? base.x : base.y) + (e >> 1) * 8 + r0 >= lim[nt][e & 1]) sc[mt][nt][e] = -INFINITY;
+            }
+            unsigned pf[2][NT][2];                     // probabilities as right operand of O^T
+            if (ok) {
+                float top[NT][2];
+                bool raise = false;
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) x = fmaxf(x, fmaxf(sc[n][2 * i], sc[n][2 * i + 1]));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                    mr[i] = fmaxf(m[i], x * j.scale);
-                }
-                if (__any_sync(0xffffffffu, mr[0] > m[0] || mr[1] > m[1])) {
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float f = m[i] > -INFINITY ? ex2_approx(m[i] - mr[i]) : 0.f;
-                        m[i] = mr[i];
-                        l[i] *= f;
-#pragma unroll
-                        for (int n = 0; n < NDB * 8; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
+                        top[nt][i] = fmaxf(fmaxf(sc[0][nt][i], sc[0][nt][2 + i]), fmaxf(sc[1][nt][i], sc[1][nt][2 + i])) * j.scale;
+                        raise = raise || top[nt][i] > m[nt][i] + ST_LAG;
                     }
+                if (__any_sync(0xffffffffu, raise)) {   // (the first keys always do)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float x = top[nt][i];
+#pragma unroll
+                            for (int q = 4; q < 32; q <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, q));
+                            const float mn = fmaxf(m[nt][i], x);
+                            const float f = m[nt][i] > -INFINITY ? ex2_approx(m[nt][i] - mn) : 0.f;
+                            m[nt][i] = mn;
+                            l[nt][i] *= f;
+#pragma unroll
+                            for (int d = 0; d < KS; ++d) { o[d][nt][i] *= f; o[d][nt][2 + i] *= f; }
+                        }
                 }
-                const float ref[2] = {m[0] > -INFINITY ? m[0] : 0.f, m[1] > -INFINITY ? m[1] : 0.f};
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float ref[2] = {m[nt][0] > -INFINITY ? m[nt][0] : 0.f, m[nt][1] > -INFINITY ? m[nt][1] : 0.f};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        sc[n][e] = ex2_approx(fmaf(sc[n][e], j.scale, -ref[e >> 1]));
-                        l[e >> 1] += sc[n][e];
-                    }
-                // ---- products with the values; the probabilities are rounded to bf16 here, their sum is not
+                    for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    unsigned a[4];
+                        for (int e = 0; e < 4; ++e) {
+                            sc[mt][nt][e] = ex2_approx(fmaf(sc[mt][nt][e], j.scale, -ref[e & 1]));
+                            l[nt][e & 1] += sc[mt][nt][e];
+                        }
+                        // rounded to bf16 for the second product; their sum is not
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const __nv_bfloat162 p = __floats2bfloat162_rn(sc[2 * ks + (q >> 1)][2 * (q & 1)], sc[2 * ks + (q >> 1)][2 * (q & 1) + 1]);
-                        a[q] = *reinterpret_cast<const unsigned*>(&p);
-                    }
-#pragma unroll
-                    for (int np = 0; np < NDB * 4; ++np) {
-                        const int key = ks * 16 + (((lane >> 3) & 1) << 3) + (lane & 7), ch = (np & 3) * 2 + (lane >> 4);
-                        unsigned bf[4];
-                        ldsm4t(vt + (np >> 2) * HALF_TILE + key * 128 + ((ch ^ (key & 7)) << 4), bf);
-                        mma16816(o[2 * np], a, bf[0], bf[1]);
-                        mma16816(o[2 * np + 1], a, bf[2], bf[3]);
+                        for (int i = 0; i < 2; ++i) {
+                            const __nv_bfloat162 p = __floats2bfloat162_rn(sc[mt][nt][2 * i], sc[mt][nt][2 * i + 1]);
+                            pf[mt][nt][i] = transposed(*reinterpret_cast<const unsigned*>(&p));
+                        }
                     }
                 }
             }
-            __syncwarp();                              // all lanes have read the slot
-            if (ok) { ++used; produce(); }
+            wait_slot(51);
+            if (ok) {
+                const int st = used % SLOTS;
+                // values of slots that hold nothing of this sequence must not meet a zero probability as NaN
+                if (base.x + 15 >= s.len || base.y + 15 >= s.len) {
+                    unsigned char* v = ring + st * st_slot_bytes<NDB>();
+                    for (int q = lane; q < GK * NDB * 8; q += 32) {
+                        const int key = (q >> 3) & 31, db = q >> 8;
+                        if ((key < 16 ? base.x + key : base.y + key - 16) >= s.len)
+                            *reinterpret_cast<uint4*>(v + db * BLOCK + key * 128 + (q & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the slot's next load comes through the async proxy)
+                    __syncwarp();
+                }
+                const unsigned vt = ring_u + st * st_slot_bytes<NDB>();
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int d = 0; d < KS; ++d) {
+                        unsigned a[4];
+                        ldsm4t(vt + (d >> 2) * BLOCK + (mt * 16 + v_key) * 128 + ((((d & 3) * 2 + v_ch) ^ (v_key & 7)) << 4), a);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma16816(o[d][nt], a, pf[mt][nt][0], pf[mt][nt][1]);
+                    }
+            }
+            release();
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-        }
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int q = 4; q < 32; q <<= 1) l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], q);
         auto out_row = [&](int row) {
             const int t = LIST ? 0 : row / G, g = s.g0 + (LIST ? row : row - t * G);
             return j.out + (int64_t)(s.row + t) * j.ldo + ((int64_t)s.head * G + g) * c.d;
         };
         if (TEAM == 1) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int row = r0 + 8 * i;
-                if (row < s.rows) {
-                    const float f = l[i] > 0.f ? 1.0f / l[i] : 0.f;
-                    __nv_bfloat16* dst = out_row(row);
+            for (int nt = 0; nt < NT; ++nt) {
+                const float f[2] = {l[nt][0] > 0.f ? 1.0f / l[nt][0] : 0.f, l[nt][1] > 0.f ? 1.0f / l[nt][1] : 0.f};
+                __nv_bfloat16* dst = out_row(nt * 8 + r0);
 #pragma unroll
-                    for (int n = 0; n < NDB * 8; ++n)
-                        if (n * 8 < c.d)
-                            *reinterpret_cast<__nv_bfloat162*>(dst + n * 8 + c0) = __floats2bfloat162_rn(o[n][2 * i] * f, o[n][2 * i + 1] * f);
-                }
+                for (int d = 0; d < KS; ++d)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const __nv_bfloat162 p = __floats2bfloat162_rn(o[d][nt][2 * i] * f[0], o[d][nt][2 * i + 1] * f[1]);
+                        const unsigned x = transposed(*reinterpret_cast<const unsigned*>(&p));   // two elements of row r0
+                        if (nt * 8 + r0 < s.rows && d * 16 < c.d) *reinterpret_cast<unsigned*>(dst + d * 16 + i * 8 + c0) = x;
+                    }
             }
             continue;
         }
-        // ---- the four warps' shares of the row tile
+        // ---- the warps' shares of the row tile, eight rows at a time
         constexpr int W = NDB * 64;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = r0 + 8 * i;
-            if (row < s.rows) {
-                if ((lane & 3) == 0) { sh.m[warp][row] = m[i]; sh.l[warp][row] = l[i]; }
-#pragma unroll
-                for (int n = 0; n < NDB * 8; ++n)
-                    *reinterpret_cast<float2*>(mrg + (warp * 16 + row) * W + n * 8 + c0) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
-            }
-        }
-        __syncthreads();
         const int col = tid % W;
         float* mine = partial<LIST>(ws, s, s.piece);
-        for (int row = tid / W; row < s.rows; row += ST_THREADS / W) {
-            float M = -INFINITY, L = 0.f, x = 0.f;
+        if (lane < 4)
 #pragma unroll
-            for (int q = 0; q < ST_WARPS; ++q) M = fmaxf(M, sh.m[q][row]);
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int q = 0; q < ST_WARPS; ++q) {
-                const float mq = sh.m[q][row], f = mq > -INFINITY ? ex2_approx(mq - M) : 0.f;
-                L = fmaf(sh.l[q][row], f, L);
-                x = fmaf(mrg[(q * 16 + row) * W + col], f, x);
+                for (int i = 0; i < 2; ++i) { sh.m[warp][nt * 8 + c0 + i] = m[nt][i]; sh.l[warp][nt * 8 + c0 + i] = l[nt][i]; }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt * 8 >= s.rows) break;
+#pragma unroll
+            for (int d = 0; d < KS; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    mrg[(warp * 8 + c0 + (e & 1)) * W + d * 16 + (e >> 1) * 8 + r0] = o[d][nt][e];
+            __syncthreads();
+            const int rows = min(s.rows - nt * 8, 8);
+            for (int rr = tid / W; rr < rows; rr += ST_THREADS / W) {
+                const int row = nt * 8 + rr;
+                float M = -INFINITY, L = 0.f, x = 0.f;
+#pragma unroll
+                for (int q = 0; q < ST_WARPS; ++q) M = fmaxf(M, sh.m[q][row]);
+#pragma unroll
+                for (int q = 0; q < ST_WARPS; ++q) {
+                    const float mq = sh.m[q][row], f = mq > -INFINITY ? ex2_approx(mq - M) : 0.f;
+                    L = fmaf(sh.l[q][row], f, L);
+                    x = fmaf(mrg[(q * 8 + rr) * W + col], f, x);
+                }
+                if (s.pieces == 1) {
+                    if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L > 0.f ? x / L : 0.f);
+                } else {
+                    mine[row * 128 + col] = x;
+                    if (col == 0) { mine[2048 + row] = M; mine[2064 + row] = L; }
+                }
             }
-            if (s.pieces == 1) {
-                if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L > 0.f ? x / L : 0.f);
-            } else {
-                mine[row * 128 + col] = x;
-                if (col == 0) { mine[2048 + row] = M; mine[2064 + row] = L; }
-            }
+            __syncthreads();                           // the buffer is reused
         }
         if (s.pieces > 1) {
             __threadfence();
@@ -515,40 +570,51 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                 __threadfence();
                 for (int row = tid / W; row < s.rows; row += ST_THREADS / W) {
                     float M = -INFINITY, L = 0.f, x = 0.f;
+                    for (int p = 0; p < s.pieces; ++p) M = fmaxf(M, __ldcg(partial<LIST>(ws, s, p) + 2048 + row));
+                    const float ref = M > -INFINITY ? M : 0.f;
+#pragma unroll 4
                     for (int p = 0; p < s.pieces; ++p) {
                         const float* part = partial<LIST>(ws, s, p);
-                        const float mp = __ldcg(part + 2048 + row), lp = __ldcg(part + 2064 + row), xp = __ldcg(part + row * 128 + col);
-                        const float Mn = fmaxf(M, mp);
-                        const float fa = M > -INFINITY ? ex2_approx(M - Mn) : 0.f, fb = mp > -INFINITY ? ex2_approx(mp - Mn) : 0.f;
-                        L = L * fa + lp * fb;
-                        x = x * fa + xp * fb;
-                        M = Mn;
+                        const float f = ex2_approx(__ldcg(part + 2048 + row) - ref);
+                        L = fmaf(__ldcg(part + 2064 + row), f, L);
+                        x = fmaf(__ldcg(part + row * 128 + col), f, x);
                     }
                     if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L > 0.f ? x / L : 0.f);
                 }
             }
+            __syncthreads();
         }
-        __syncthreads();                               // the merge buffer is reused
     }
     // a warp that gave up has copies in flight: they have to land before its shared memory goes
     if (!ok) {
         for (unsigned i = used; i < made; ++i) {
             const unsigned long long t0 = global_ns();
-            while (!mbar_try(&sh.full[warp][i % NST], (i / NST) & 1u))
+            while (!mbar_try(&sh.full[warp][i % SLOTS], (i / SLOTS) & 1u))
                 if (past_limit(2 * (global_ns() - t0), abort_flag)) break;
         }
         if (lane == 0) { atomicOr(status, ST_TIMEOUT); status[2] = 300u + (unsigned)abort_flag[0]; }
     }
 }
 
-template <int NDB, bool LIST, int TEAM>
-cudaError_t run_step(ada_ctx* ctx, const StepMaps& maps, const CacheView& c, const Ragged& r, const AttendJob& j, int grid,
-                     int tiles, int pieces, cudaStream_t s) {
-    auto kernel = k_cache_step<NDB, LIST, TEAM>;
+struct StepPlan {
+    int grid, tiles, pieces;
+};
+
+template <int NDB, int NT, bool LIST, int TEAM>
+cudaError_t run_step(ada_ctx* ctx, const StepMaps& maps, const CacheView& c, const Ragged& r, const AttendJob& j,
+                     const StepPlan& p, cudaStream_t s) {
+    auto kernel = k_cache_step<NDB, NT, LIST, TEAM>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, st_smem<NDB>());
     if (e != cudaSuccess) return e;
-    return launch_k(ctx, kernel, dim3(grid), dim3(ST_THREADS), st_smem<NDB>(), s, maps, c, r, j, tiles, pieces,
+    return launch_k(ctx, kernel, dim3(p.grid), dim3(ST_THREADS), st_smem<NDB>(), s, maps, c, r, j, p.tiles, p.pieces,
                     ctx->cache_part, ctx->cache_ctr, ctx->status);
+}
+template <bool LIST, int TEAM>
+cudaError_t run_step(ada_ctx* ctx, const StepMaps& maps, const CacheView& c, const Ragged& r, const AttendJob& j,
+                     const StepPlan& p, int rows, cudaStream_t s) {
+    if (c.d > 64)
+        return rows <= 8 ? run_step<2, 1, LIST, TEAM>(ctx, maps, c, r, j, p, s) : run_step<2, 2, LIST, TEAM>(ctx, maps, c, r, j, p, s);
+    return rows <= 8 ? run_step<1, 1, LIST, TEAM>(ctx, maps, c, r, j, p, s) : run_step<1, 2, LIST, TEAM>(ctx, maps, c, r, j, p, s);
 }
 
 }  // namespace
@@ -558,25 +624,20 @@ cudaError_t launch_cache_step(ada_ctx* ctx, const CacheView& c, const Ragged& r,
     const int box = c.shift == 4 ? 16 : GK;
     if (!encode_pages(&maps.k, c, c.k, box) || !encode_pages(&maps.v, c, c.v, box)) return cudaErrorInvalidValue;
     const int G = j.h / c.h_kv;
-    const bool wide = c.d > 64;
-    if (j.blk_idx == nullptr)
-        return wide ? run_step<2, false, 4>(ctx, maps, c, r, j, ctx->sm_count, 1, 1, s)
-                    : run_step<1, false, 4>(ctx, maps, c, r, j, ctx->sm_count, 1, 1, s);
-    const int tiles = (G + 15) / 16;
-    const int64_t rows = (int64_t)r.N * c.h_kv * tiles;
-    // rows enough for every warp of the GPU: a warp each, nothing to join
-    if (rows >= 4 * (int64_t)ctx->sm_count)
-        return wide ? run_step<2, true, 1>(ctx, maps, c, r, j, ctx->sm_count, tiles, 1, s)
-                    : run_step<1, true, 1>(ctx, maps, c, r, j, ctx->sm_count, tiles, 1, s);
-    // few rows: their lists are cut into pieces of at least 4 granules for each warp, as many as fill the SMs
-    const int64_t room = ((int64_t)j.k << c.shift) / (4 * ST_WARPS * GK);
+    StepPlan p = {ctx->sm_count, 1, 1};
+    if (j.blk_idx == nullptr) return run_step<false, ST_WARPS>(ctx, maps, c, r, j, p, j.max_new * G, s);
+    p.tiles = (G + 15) / 16;
+    const int64_t rows = (int64_t)r.N * c.h_kv * p.tiles;
+    // row tiles enough for every warp of the GPU: a warp each, nothing to join
+    if (rows >= ST_WARPS * (int64_t)ctx->sm_count) return run_step<true, 1>(ctx, maps, c, r, j, p, G, s);
+    // few of them: their lists are cut into pieces of at least 4 granules for each warp, as many as fill the SMs
+    const int64_t room = ((int64_t)j.k << c.shift) / (4 * UNIT);
     int64_t pieces = (2 * ctx->sm_count) / rows;
     pieces = pieces < room ? pieces : room;
-    pieces = pieces < 1 ? 1 : pieces;
-    const int64_t items = rows * pieces;
-    const int grid = (int)(items < ctx->sm_count ? items : ctx->sm_count);
-    return wide ? run_step<2, true, 4>(ctx, maps, c, r, j, grid, tiles, (int)pieces, s)
-                : run_step<1, true, 4>(ctx, maps, c, r, j, grid, tiles, (int)pieces, s);
+    p.pieces = pieces < 1 ? 1 : (int)pieces;
+    const int64_t items = rows * p.pieces;
+    if (items < p.grid) p.grid = (int)items;
+    return run_step<true, ST_WARPS>(ctx, maps, c, r, j, p, G, s);
 }
 
 }  // namespace ada

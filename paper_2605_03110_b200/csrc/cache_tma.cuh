@@ -38,6 +38,13 @@ static __device__ __forceinline__ void mma16816(float (&c)[4], const unsigned (&
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// transposes an 8 x 8 matrix of 16-bit elements held as a matrix fragment (two elements of a row per lane)
+static __device__ __forceinline__ unsigned transposed(unsigned x) {
+    unsigned y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
 // (element, slot, head, page): boxes of 64 elements x `box_rows` slots of one head and page, 128-byte swizzle
 static inline bool encode_pages(CUtensorMap* map, const CacheView& c, const void* base, int box_rows) {
     EncodeTiledFn fn = encode_fn();
