@@ -92,13 +92,23 @@ ada_status ada_attention_cached(ada_ctx* ctx, const ada_kv_cache* cache, int64_t
     j.Q = static_cast<const __nv_bfloat16*>(Q); j.ldq = ldq;
     j.out = static_cast<__nv_bfloat16*>(out); j.ldo = ldo;
     j.h = (int)h; j.max_new = (int)(max_new < N ? max_new : N); j.causal = (flags & ADA_ATTN_CAUSAL) ? 1 : 0;
-    j.blk_idx = j.blk_cnt = nullptr; j.k = 0;
+    j.blk_idx = j.blk_cnt = nullptr; j.k = 0; j.few = 0;
     DeviceGuard guard(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     CU(ensure_cache_ws(ctx, s));
-    // rows of a key head that one 16-row tile of mma.sync holds, or tiles of 128 rows
-    if ((int64_t)j.max_new * (h / c.h_kv) <= 16) CU(launch_cache_step(ctx, c, r, j, s));
-    else CU(launch_cache_chunk(ctx, c, r, j, s));
+    // rows of a key head that one 16-row tile of mma.sync holds, or tiles of 128 rows; several sequences may be mixed
+    const int few = 16 / (j.h / c.h_kv);
+    if (j.max_new <= few) {
+        CU(launch_cache_step(ctx, c, r, j, s));
+        return ADA_OK;
+    }
+    if (r.B > 1 && few > 0) {
+        j.few = few;
+        AttendJob step = j;
+        step.max_new = few;
+        CU(launch_cache_step(ctx, c, r, step, s));
+    }
+    CU(launch_cache_chunk(ctx, c, r, j, s));
     return ADA_OK;
 }
 
@@ -138,7 +148,7 @@ ada_status ada_attention_blocks(ada_ctx* ctx, const ada_kv_cache* cache, int64_t
     j.Q = static_cast<const __nv_bfloat16*>(Q); j.ldq = ldq;
     j.out = static_cast<__nv_bfloat16*>(out); j.ldo = ldo;
     j.h = (int)h; j.max_new = 1; j.causal = (flags & ADA_ATTN_CAUSAL) ? 1 : 0;
-    j.blk_idx = blk_idx; j.blk_cnt = blk_cnt; j.k = (int)k;
+    j.blk_idx = blk_idx; j.blk_cnt = blk_cnt; j.k = (int)k; j.few = 0;
     DeviceGuard guard(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     CU(ensure_cache_ws(ctx, s));

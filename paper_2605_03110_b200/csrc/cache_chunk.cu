@@ -5,9 +5,9 @@
 // of TMEM: two score tiles, two accumulators) are a CTA's work item, and both read the same tiles of 128 keys.
 //   warp 0      TMA: queries, and pages of K and V into a ring of slots (one slot = K or V of 128 keys)
 //   warp 1      tcgen05.mma: S_t = Q_t K^T, O_t += P_t V; while tile 0's softmax runs, tile 1's products do
-//   warps 2..5  softmax of tile 0, one row per thread: S out of TMEM into registers, 2^(s - m), P back into TMEM as bf16
+//   warps 4..7  softmax of tile 0, one row per thread: S out of TMEM into registers, 2^(s - m), P back into TMEM as bf16
 //               over its own scores, where the second product takes it from as its left operand
-//   warps 6..9  the same for tile 1
+//   warps 8..11 the same for tile 1 (they have most of the registers: a row's 128 scores stay in them)
 // V needs no transposed copy: its tiles are MN-major right operands as the pages hold them.
 // A row's reference maximum m is raised only when the running maximum has left it by more than 8 powers of two
 // (then the accumulator is rescaled in TMEM); O / l does not depend on it.
@@ -23,7 +23,7 @@ using namespace tc;
 
 namespace {
 
-constexpr int CH_THREADS = 320;
+constexpr int CH_THREADS = 384;
 constexpr int CH_KEYS = 128;                      // keys per tile
 constexpr int BLK_BYTES = 128 * BK * 2;           // 128 rows x 64 elements: 16 KiB
 constexpr float CH_LAG = 8.0f;
@@ -32,7 +32,7 @@ constexpr int PART_FLOATS = 256 * 128 + 2 * 256;  // one item's partial result: 
 template <int NDB> __host__ __device__ constexpr int ch_slots() { return 10 / NDB; }
 
 struct ChunkShared {
-    unsigned long long q_full, q_empty, full[10], empty[10], s_full[2], p_full[2], o_full[2], o_empty[2];
+    unsigned long long q_full, q_empty, full[10], empty[10], s_full[2], p_full[2][2], o_full[2], o_empty[2];
     unsigned tmem_base;
     int abort_flag[2];
     int start[4];                                 // b, p, head, ku of the CTA's first unit
@@ -66,12 +66,16 @@ struct ChunkWork {
     static __device__ __forceinline__ int units(int n, int len, int p, int tq, int causal) {
         return max((limit(n, len, (p + 1) * 2 * tq, causal) + CH_KEYS - 1) / CH_KEYS, 1);
     }
-    __device__ __forceinline__ void load_seq(const Ragged& r, const CacheView& c, int tq, int max_new) {
+    // items of a sequence of n new tokens: none if it is the other kernel's
+    static __device__ __forceinline__ int items(int n, int tq, int max_new, int few) {
+        return n <= few ? 0 : (min(n, max_new) + 2 * tq - 1) / (2 * tq);
+    }
+    __device__ __forceinline__ void load_seq(const Ragged& r, const CacheView& c, int tq, int max_new, int few) {
         n = seq_rows(r, b, off);
         len = seq_len(r, c, b);
-        P = (min(n, max_new) + 2 * tq - 1) / (2 * tq);
+        P = items(n, tq, max_new, few);
     }
-    __device__ __forceinline__ bool next(Item& it, const Ragged& r, const CacheView& c, int tq, int causal, int max_new) {
+    __device__ __forceinline__ bool next(Item& it, const Ragged& r, const CacheView& c, int tq, int causal, int max_new, int few) {
         if (at >= end) return false;
         while (P == 0 || ku >= nu) {
             ku = 0;
@@ -80,7 +84,7 @@ struct ChunkWork {
                 if (P == 0 || ++p >= P) {
                     p = 0;
                     if (++b >= r.B) { at = end; return false; }
-                    load_seq(r, c, tq, max_new);
+                    load_seq(r, c, tq, max_new, few);
                     if (P == 0) continue;
                 }
                 nu = units(n, len, p, tq, causal);
@@ -128,6 +132,74 @@ __device__ __forceinline__ unsigned long long smem_desc_mn(unsigned addr) {
     return d;
 }
 
+__device__ __forceinline__ float max3(float a, unsigned b, unsigned c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+    return d;
+}
+__device__ __forceinline__ unsigned long long pack2(float a, float b) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(unsigned long long v, float& a, float& b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// p = 2^(x scale + nref) of 64 scores, as bf16 pairs; their sum.  The special-function unit takes 8 cycles for a warp's
+// 32 exponentials, as long as everything else in this loop: CH_POLY of every 8 pairs go through the multipliers
+// instead: y = n + f with n the nearest integer (left in the low bits by adding 1.5 x 2^23), 2^f on [-1/2, 1/2] a cubic
+// that is off by at most 7.5e-5 of itself (fitted for least relative error; a bf16 is rounded by up to 3.9e-3), n
+// added to the exponent.  Arguments below -126 give 2^-126.  With masked scores (-inf, to give 0) all take the unit.
+constexpr int CH_POLY = 3;
+template <bool MASKED>
+__device__ __forceinline__ void exp_pairs(const unsigned (&a)[32], const unsigned (&b)[32], float scale, float nref,
+                                          unsigned (&w)[32], float2& sum) {
+    const unsigned long long sc2 = pack2(scale, scale), nr2 = pack2(nref, nref);
+    const unsigned long long big = pack2(12582912.f, 12582912.f), nbig = pack2(-12582912.f, -12582912.f);
+    const unsigned long long neg = pack2(-1.f, -1.f);
+    const unsigned long long c0 = pack2(0.99992806f, 0.99992806f), c1 = pack2(0.69326097f, 0.69326097f),
+                             c2 = pack2(0.24261113f, 0.24261113f), c3 = pack2(0.05517167f, 0.05517167f);
+    unsigned long long s2[2] = {pack2(sum.x, 0.f), pack2(sum.y, 0.f)};
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const unsigned (&x)[32] = i < 16 ? a : b;
+        const int e = 2 * (i & 15);
+        const unsigned long long y2 = fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), sc2, nr2);
+        float p0, p1;
+        unpack2(y2, p0, p1);
+        if (!MASKED && (i & 7) < CH_POLY) {
+            const unsigned long long y = pack2(fmaxf(p0, -126.f), fmaxf(p1, -126.f));
+            const unsigned long long t = add2(y, big), f = fma2(add2(t, nbig), neg, y);
+            const unsigned long long q = fma2(fma2(fma2(c3, f, c2), f, c1), f, c0);
+            float t0, t1;
+            unpack2(t, t0, t1);
+            unpack2(q, p0, p1);
+            p0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
+            p1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
+        } else {
+            p0 = ex2_approx(p0);
+            p1 = ex2_approx(p1);
+        }
+        s2[i & 1] = add2(s2[i & 1], pack2(p0, p1));
+        const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
+        w[i] = *reinterpret_cast<const unsigned*>(&h);
+    }
+    float u0, u1, v0, v1;
+    unpack2(s2[0], u0, u1);
+    unpack2(s2[1], v0, v1);
+    sum = make_float2(u0 + u1, v0 + v1);
+}
+
 template <int NDB>
 __global__ void __launch_bounds__(CH_THREADS, 1)
 k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const Ragged r, const AttendJob j, int tq,
@@ -150,7 +222,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
         mbar_init(&sh.q_full, 1); mbar_init(&sh.q_empty, 1);
         for (int i = 0; i < SLOTS; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
         for (int t = 0; t < 2; ++t) {
-            mbar_init(&sh.s_full[t], 1); mbar_init(&sh.p_full[t], 4);
+            mbar_init(&sh.s_full[t], 1); mbar_init(&sh.p_full[t][0], 4); mbar_init(&sh.p_full[t][1], 4);
             mbar_init(&sh.o_full[t], 1); mbar_init(&sh.o_empty[t], 4);
         }
         sh.abort_flag[0] = 0;
@@ -173,7 +245,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
             int o;
             const int n = seq_rows(r, b, o), len = seq_len(r, c, b);
             if (blockIdx.x == 0 && n > j.max_new) atomicOr(status, ST_BAD_COUNT);
-            const int P = (min(n, j.max_new) + 2 * tq - 1) / (2 * tq);
+            const int P = ChunkWork::items(n, tq, j.max_new, j.few);
             int u = 0;
             for (int p = 0; p < P; ++p) u += ChunkWork::units(n, len, p, tq, j.causal);
             return u;
@@ -238,11 +310,13 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
     work.b = sh.start[0]; work.p = sh.start[1]; work.head = sh.start[2]; work.ku = sh.start[3];
     work.n = work.off = work.len = work.nu = work.P = 0;
     if (work.at < work.end) {
-        work.load_seq(r, c, tq, j.max_new);
+        work.load_seq(r, c, tq, j.max_new, j.few);
         work.nu = ChunkWork::units(work.n, work.len, work.p, tq, j.causal);
     }
     Item it;
-
+    // Registers: 384 x 168 at launch = 128 x 72 + 256 x 216.  (Inside the roles' branches: where they meet the compiler
+    // has to assume the smaller number.)
+    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
         // ------------------------------------------------ TMA producer
         bool ok = true;
@@ -250,12 +324,12 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
         const int np = CH_KEYS >> min(c.shift, 7); // pages per key tile
         const int ps = 1 << c.shift;
         int k = 0;                                 // items
-        for (; ok && work.next(it, r, c, tq, j.causal, j.max_new); ++k) {
+        for (; ok && work.next(it, r, c, tq, j.causal, j.max_new, j.few); ++k) {
             if (k > 0) ok = mbar_wait(&sh.q_empty, (unsigned)(k - 1) & 1u, abort_flag, 30);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;                        // (k items' queries have been asked for)
             const int two = it.units[1] > 0 ? 2 : 1;
-            if (lane == 0) {
+            if (elect_one()) {
                 mbar_expect_tx(&sh.q_full, (unsigned)(two * NDB * tq * G * 128));
                 for (int t = 0; t < two; ++t)
                     for (int db = 0; db < NDB; ++db)
@@ -296,13 +370,13 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     if (past_limit(2 * (global_ns() - t0), abort_flag)) { *abort_flag = 33; break; }
         }
     } else if (warp == 1) {
-        // ------------------------------------------------ MMA issuer (lane 0; all lanes follow)
+        // ------------------------------------------------ MMA issuer (one lane; all lanes follow)
         bool ok = true;
         unsigned got = 0;                          // slots consumed
         unsigned n_p[2] = {0u, 0u}, n_o[2] = {0u, 0u};
         const unsigned idesc_s = instr_desc(CH_KEYS);
         const unsigned idesc_o = instr_desc(NDB * 64) | (1u << 16);          // right operand MN-major
-        for (int k = 0; ok && work.next(it, r, c, tq, j.causal, j.max_new); ++k) {
+        for (int k = 0; ok && work.next(it, r, c, tq, j.causal, j.max_new, j.few); ++k) {
             const int nt[2] = {ChunkWork::tiles_of(it, 0), ChunkWork::tiles_of(it, 1)};
             const int two = it.units[1] > 0 ? 2 : 1;
             ok = mbar_wait(&sh.q_full, (unsigned)k & 1u, abort_flag, 35);
@@ -319,7 +393,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
             wait_slot(got, 36);
             if (!ok) break;
             tcgen05_fence_after();
-            if (lane == 0) {
+            if (elect_one()) {
                 for (int t = 0; t < two; ++t)
                     if (nt[t] > 0) issue_s(t, got);
                 umma_commit(&sh.empty[got % SLOTS]);
@@ -345,41 +419,47 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 if (!ok) break;
                 for (int t = 0; t < two; ++t) {
                     if (u >= nt[t]) continue;
-                    ok = mbar_wait(&sh.p_full[t], n_p[t] & 1u, abort_flag, 39);
-                    ++n_p[t];
                     // the accumulator is overwritten: the previous item's rows have been read out
-                    if (u == 0 && n_o[t] > 0) ok = ok && mbar_wait(&sh.o_empty[t], (n_o[t] - 1u) & 1u, abort_flag, 40);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    tcgen05_fence_after();
-                    if (lane == 0) {
-                        const unsigned long long b = smem_desc_mn(smem_u32(ring + (sv % SLOTS) * SLOT_BYTES));
+                    if (u == 0 && n_o[t] > 0) ok = mbar_wait(&sh.o_empty[t], (n_o[t] - 1u) & 1u, abort_flag, 40);
+                    const unsigned long long b = smem_desc_mn(smem_u32(ring + (sv % SLOTS) * SLOT_BYTES));
 #pragma unroll
-                        for (int q = 0; q < CH_KEYS / UMMA_K; ++q)
-                            umma_ts(tmem_base + 256 + t * 128, tmem_base + t * 128 + q * 8, b + q * (2048 >> 4), idesc_o, (u | q) != 0);
+                    for (int h = 0; h < 2; ++h) {                            // as soon as half of the probabilities are there
+                        ok = ok && mbar_wait(&sh.p_full[t][h], n_p[t] & 1u, abort_flag, 39);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        tcgen05_fence_after();
+                        if (elect_one())
+#pragma unroll
+                            for (int q = 4 * h; q < 4 * h + 4; ++q)
+                                umma_ts(tmem_base + 256 + t * 128, tmem_base + t * 128 + q * 8, b + q * (2048 >> 4), idesc_o, (u | q) != 0);
+                    }
+                    if (!ok) break;
+                    ++n_p[t];
+                    if (elect_one()) {
                         if (u + 1 < nt[t]) issue_s(t, sk);
                         else umma_commit(&sh.o_full[t]);
                     }
                     if (u + 1 >= nt[t]) ++n_o[t];
                 }
                 if (!ok) break;
-                if (lane == 0) {
+                if (elect_one()) {
                     umma_commit(&sh.empty[sv % SLOTS]);
                     if (ahead) umma_commit(&sh.empty[sk % SLOTS]);
                     if (u + 2 == it.take) umma_commit(&sh.q_empty);   // the item's last scores are under way
                 }
             }
         }
-    } else {
+    } else if (warp >= 4) {
         // ------------------------------------------------ softmax and output
-        const int quad = warp & 3, t = (warp - 2) >> 2;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int quad = warp & 3, t = (warp - 4) >> 2;
         const int i = quad * 32 + lane;                                     // row of the tile
         const unsigned t_s = tmem_base + ((unsigned)(quad * 32) << 16) + t * 128;
         const unsigned t_o = t_s + 256;
         const int tok = i / G, g = i - tok * G;                             // within the tile
         bool ok = true;
         unsigned n_s = 0, n_o = 0;
-        while (work.next(it, r, c, tq, j.causal, j.max_new)) {
+        while (work.next(it, r, c, tq, j.causal, j.max_new, j.few)) {
             if (it.units[t] == 0 && t == 1) continue;                       // no rows in this tile
             const int nt = ChunkWork::tiles_of(it, t);
             const int tok_i = t * tq + tok;                                 // within the item
@@ -394,23 +474,28 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 ++n_s;
                 tcgen05_fence_after();
                 unsigned x[4][32];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_ld32_issue(t_s + q * 32, x[q]);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_ld_wait(x[q]);
                 const int k0 = (it.ku + u) * CH_KEYS;
-                if (k0 + CH_KEYS > lim_tile) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                const bool masked = k0 + CH_KEYS > lim_tile;
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto most = [&](unsigned (&y)[32], int at) {                // (mask and) maximum of 32 scores
+                    if (masked) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if (k0 + q * 32 + e >= lim) x[q][e] = 0xff800000u;
-                }
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                            if (at + e >= lim) y[e] = 0xff800000u;
+                    }
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(x[q][e]));
+                    for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], y[e], y[e + 1]);
+                };
+                tmem_ld32_issue(t_s, x[0]);
+                tmem_ld32_issue(t_s + 32, x[1]);
+                tmem_ld_wait(x[0]); tmem_ld_wait(x[1]);
+                tmem_ld32_issue(t_s + 64, x[2]);
+                tmem_ld32_issue(t_s + 96, x[3]);
+                most(x[0], k0);
+                most(x[1], k0 + 32);
+                tmem_ld_wait(x[2]); tmem_ld_wait(x[3]);
+                most(x[2], k0 + 64);
+                most(x[3], k0 + 96);
                 const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * j.scale);
                 if (u == 0) {
                     m = m_new;
@@ -433,27 +518,18 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     }
                 }
                 const float ref = m > -INFINITY ? m : 0.f;
-                float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+                float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int h2 = 0; h2 < 2; ++h2) {
+                for (int h = 0; h < 2; ++h) {
                     unsigned w[32];
-#pragma unroll
-                    for (int e = 0; e < 64; e += 4) {
-                        const float p0 = ex2_approx(fmaf(__uint_as_float(x[2 * h2 + (e >> 5)][e & 31]), j.scale, -ref));
-                        const float p1 = ex2_approx(fmaf(__uint_as_float(x[2 * h2 + (e >> 5)][(e & 31) + 1]), j.scale, -ref));
-                        const float p2 = ex2_approx(fmaf(__uint_as_float(x[2 * h2 + (e >> 5)][(e & 31) + 2]), j.scale, -ref));
-                        const float p3 = ex2_approx(fmaf(__uint_as_float(x[2 * h2 + (e >> 5)][(e & 31) + 3]), j.scale, -ref));
-                        s0 += p0; s1 += p1; s2 += p2; s3 += p3;
-                        const __nv_bfloat162 lo = __floats2bfloat162_rn(p0, p1), hi = __floats2bfloat162_rn(p2, p3);
-                        w[e >> 1] = *reinterpret_cast<const unsigned*>(&lo);
-                        w[(e >> 1) + 1] = *reinterpret_cast<const unsigned*>(&hi);
-                    }
-                    tmem_st32(t_s + h2 * 32, w);
+                    if (masked) exp_pairs<true>(x[2 * h], x[2 * h + 1], j.scale, -ref, w, sum);
+                    else exp_pairs<false>(x[2 * h], x[2 * h + 1], j.scale, -ref, w, sum);
+                    tmem_st32(t_s + h * 32, w);
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.p_full[t][h]);
                 }
-                l += (s0 + s1) + (s2 + s3);
-                tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.p_full[t]);
+                l += sum.x + sum.y;
             }
             if (!ok) break;
             // ---- the item's rows
@@ -524,23 +600,34 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                         L = fmaf(__ldcg(o + 256), ex2_approx(__ldcg(o) - Mr), L);
                     }
                     const float f = L > 0.f ? 1.0f / L : 0.f;
-                    for (int q = 0; q < NDB * 8; ++q) {
-                        if (q * 8 >= c.d) break;
-                        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                    for (int q = 0; q < NDB * 2; ++q) {                      // 32 columns of a piece in flight
+                        if (q * 32 >= c.d) break;
+                        float y[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) y[e] = 0.f;
+#pragma unroll 1
                         for (int p = 0; p < it.pieces; ++p) {
                             const float* o = part(p) + t * 128 + i;
                             const float fp = ex2_approx(__ldcg(o + 128 * 256) - Mr);
+                            float z[32];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) y[e] = fmaf(__ldcg(o + (q * 8 + e) * 256), fp, y[e]);
+                            for (int e = 0; e < 32; ++e) z[e] = __ldcg(o + (q * 32 + e) * 256);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) y[e] = fmaf(z[e], fp, y[e]);
                         }
                         if (live) {
-                            unsigned w[4];
 #pragma unroll
-                            for (int v = 0; v < 4; ++v) {
-                                const __nv_bfloat162 p = __floats2bfloat162_rn(y[2 * v] * f, y[2 * v + 1] * f);
-                                w[v] = *reinterpret_cast<const unsigned*>(&p);
-                            }
-                            *reinterpret_cast<uint4*>(dst + q * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+                            for (int e = 0; e < 32; e += 8)
+                                if (q * 32 + e < c.d) {
+                                    unsigned w[4];
+#pragma unroll
+                                    for (int v = 0; v < 4; ++v) {
+                                        const __nv_bfloat162 h = __floats2bfloat162_rn(y[e + 2 * v] * f, y[e + 2 * v + 1] * f);
+                                        w[v] = *reinterpret_cast<const unsigned*>(&h);
+                                    }
+                                    *reinterpret_cast<uint4*>(dst + q * 32 + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                                }
                         }
                     }
                 }

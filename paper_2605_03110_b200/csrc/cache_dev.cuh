@@ -102,6 +102,8 @@ struct AttendJob {
     __nv_bfloat16* out;
     int64_t ldo;
     int h, max_new, causal;
+    int few;                            // > 0: sequences of up to `few` new tokens are cache_step's, the others
+                                        // cache_chunk's; 0: all of them are whose kernel is called
     float scale;                        // of the scores, times log2(e)
     const int32_t *blk_idx, *blk_cnt;   // [N][h_kv][k], [N][h_kv]; NULL: every page
     int k;

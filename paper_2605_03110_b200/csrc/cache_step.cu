@@ -73,10 +73,10 @@ struct Work {                              // where a team is in its run of work
     int64_t per;
     int row, rt, piece;                    // lists
 
-    __device__ __forceinline__ void load_seq(const Ragged& r, const CacheView& c) {
+    __device__ __forceinline__ void load_seq(const Ragged& r, const CacheView& c, int few) {
         n = seq_rows(r, b, off);
         len = seq_len(r, c, b);
-        nu = n > 0 ? max(1, (len + UNIT - 1) / UNIT) : 0;
+        nu = n > 0 && !(few > 0 && n > few) ? max(1, (len + UNIT - 1) / UNIT) : 0;
     }
     // the next segment, or false
     __device__ __forceinline__ bool next(Seg& s, const Ragged& r, const CacheView& c, const AttendJob& j, int G, int tiles,
@@ -86,7 +86,7 @@ struct Work {                              // where a team is in its run of work
                 if (b < 0 || row < off || row >= off + n) {     // another sequence
                     b = seq_of_row(r, row);
                     if (b < 0) { at = end; return false; }      // (rows of no sequence come last)
-                    load_seq(r, c);
+                    load_seq(r, c, j.few);
                 }
                 s.b = b; s.head = head; s.row = row; s.g0 = rt * 16;
                 s.rows = min(16, G - rt * 16);
@@ -117,7 +117,7 @@ struct Work {                              // where a team is in its run of work
             if (++head >= c.h_kv || nu == 0) {
                 head = 0;
                 if (++b >= r.B) { at = end; return false; }
-                load_seq(r, c);
+                load_seq(r, c, j.few);
             }
         }
         const int take = (int)min((int64_t)(nu - ku), end - at);
@@ -208,6 +208,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
             if (b >= r.B) return 0;
             int o;
             const int n = seq_rows(r, b, o);
+            if (j.few > 0 && n > j.few) return 0;
             if (blockIdx.x == 0 && n > j.max_new) atomicOr(status, ST_BAD_COUNT);
             return n > 0 ? max(1, (seq_len(r, c, b) + UNIT - 1) / UNIT) : 0;
         };
@@ -232,7 +233,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                     const int l = __ffs(hit) - 1;
                     before += __shfl_sync(0xffffffffu, sum - own, l);
                     work.b = b0 + l;
-                    work.load_seq(r, c);
+                    work.load_seq(r, c, j.few);
                     const int64_t rest = work.at - before * c.h_kv;
                     work.head = (int)(rest / work.nu);
                     work.ku = (int)(rest % work.nu);
@@ -301,12 +302,12 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
             const int l = (pg - batch) / TEAM;
             id0 = __shfl_sync(0xffffffffu, pid.x, l); id1 = __shfl_sync(0xffffffffu, pid.y, l);
             const int b0 = __shfl_sync(0xffffffffu, pbase.x, l), b1 = __shfl_sync(0xffffffffu, pbase.y, l);
-            if (lane == 0) sh.base[warp][made % SLOTS] = make_int2(b0, b1);
+            if (elect_one()) sh.base[warp][made % SLOTS] = make_int2(b0, b1);
             first_slot = (pg * GK) & ((1 << c.shift) - 1);
             phead = ps.head;
             pg += TEAM;
         }
-        if (lane == 0) {
+        if (elect_one()) {
             const int st = made % SLOTS;
             unsigned char* dst = ring + st * st_slot_bytes<NDB>();
             unsigned long long* bar = &sh.full[warp][st];
