@@ -27,7 +27,7 @@ constexpr int CH_THREADS = 384;
 constexpr int CH_KEYS = 128;                      // keys per tile
 constexpr int BLK_BYTES = 128 * BK * 2;           // 128 rows x 64 elements: 16 KiB
 constexpr float CH_LAG = 8.0f;
-constexpr int PART_FLOATS = 256 * 128 + 2 * 256;  // one item's partial result: columns x rows, maxima, sums
+constexpr int PART_FLOATS = 256 * 128 + 2 * 256;  // one item's partial result: 4 columns x rows x 32, maxima, sums
 
 template <int NDB> __host__ __device__ constexpr int ch_slots() { return 10 / NDB; }
 
@@ -111,27 +111,6 @@ struct ChunkWork {
     static __device__ __forceinline__ int tiles_of(const Item& it, int t) { return max(min(it.units[t] - it.ku, it.take), 0); }
 };
 
-// O += P V with P in TMEM: 16 keys per instruction, V as an MN-major tile (64-element blocks of 128 keys x 128 bytes)
-__device__ __forceinline__ void umma_ts(unsigned tmem_d, unsigned tmem_a, unsigned long long bdesc, unsigned idesc,
-                                        unsigned accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-// MN-major tile, 128-byte swizzle: 8 keys are 1024 bytes, the next 64 elements of a row BLK_BYTES further on
-__device__ __forceinline__ unsigned long long smem_desc_mn(unsigned addr) {
-    unsigned long long d = 0;
-    d |= (unsigned long long)((addr & 0x3FFFFu) >> 4);
-    d |= (unsigned long long)(BLK_BYTES >> 4) << 16;
-    d |= (unsigned long long)(1024 >> 4) << 32;
-    d |= (unsigned long long)1 << 46;
-    d |= (unsigned long long)2 << 61;
-    return d;
-}
-
 __device__ __forceinline__ float max3(float a, unsigned b, unsigned c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
@@ -158,18 +137,17 @@ __device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigne
 // p = 2^(x scale + nref) of 64 scores, as bf16 pairs; their sum.  The special-function unit takes 8 cycles for a warp's
 // 32 exponentials, as long as everything else in this loop: CH_POLY of every 8 pairs go through the multipliers
 // instead: y = n + f with n the nearest integer (left in the low bits by adding 1.5 x 2^23), 2^f on [-1/2, 1/2] a cubic
-// that is off by at most 7.5e-5 of itself (fitted for least relative error; a bf16 is rounded by up to 3.9e-3), n
-// added to the exponent.  Arguments below -126 give 2^-126.  With masked scores (-inf, to give 0) all take the unit.
-constexpr int CH_POLY = 3;
-template <bool MASKED>
+// that is off by at most 1.02e-4 of itself (fitted for least relative error with a value of exactly 1 at 0; a bf16 is
+// rounded by up to 3.9e-3), n added to the exponent.  Arguments are cut at -127, where exactly 0 comes out: for masked
+// scores too.
+constexpr int CH_POLY = 2;
 __device__ __forceinline__ void exp_pairs(const unsigned (&a)[32], const unsigned (&b)[32], float scale, float nref,
-                                          unsigned (&w)[32], float2& sum) {
+                                          unsigned (&w)[32], float& sum) {
     const unsigned long long sc2 = pack2(scale, scale), nr2 = pack2(nref, nref);
     const unsigned long long big = pack2(12582912.f, 12582912.f), nbig = pack2(-12582912.f, -12582912.f);
-    const unsigned long long neg = pack2(-1.f, -1.f);
-    const unsigned long long c0 = pack2(0.99992806f, 0.99992806f), c1 = pack2(0.69326097f, 0.69326097f),
-                             c2 = pack2(0.24261113f, 0.24261113f), c3 = pack2(0.05517167f, 0.05517167f);
-    unsigned long long s2[2] = {pack2(sum.x, 0.f), pack2(sum.y, 0.f)};
+    const unsigned long long neg = pack2(-1.f, -1.f), c0 = pack2(1.f, 1.f);
+    const unsigned long long c1 = pack2(0.6932829f, 0.6932829f), c2 = pack2(0.24221095f, 0.24221095f), c3 = pack2(0.055008933f, 0.055008933f);
+    unsigned long long s2[2] = {0ull, 0ull};
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
         const unsigned (&x)[32] = i < 16 ? a : b;
@@ -177,8 +155,8 @@ __device__ __forceinline__ void exp_pairs(const unsigned (&a)[32], const unsigne
         const unsigned long long y2 = fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), sc2, nr2);
         float p0, p1;
         unpack2(y2, p0, p1);
-        if (!MASKED && (i & 7) < CH_POLY) {
-            const unsigned long long y = pack2(fmaxf(p0, -126.f), fmaxf(p1, -126.f));
+        if ((i & 7) < CH_POLY) {
+            const unsigned long long y = pack2(fmaxf(p0, -127.f), fmaxf(p1, -127.f));
             const unsigned long long t = add2(y, big), f = fma2(add2(t, nbig), neg, y);
             const unsigned long long q = fma2(fma2(fma2(c3, f, c2), f, c1), f, c0);
             float t0, t1;
@@ -197,7 +175,7 @@ __device__ __forceinline__ void exp_pairs(const unsigned (&a)[32], const unsigne
     float u0, u1, v0, v1;
     unpack2(s2[0], u0, u1);
     unpack2(s2[1], v0, v1);
-    sum = make_float2(u0 + u1, v0 + v1);
+    sum += (u0 + u1) + (v0 + v1);
 }
 
 template <int NDB>
@@ -370,10 +348,11 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     if (past_limit(2 * (global_ns() - t0), abort_flag)) { *abort_flag = 33; break; }
         }
     } else if (warp == 1) {
-        // ------------------------------------------------ MMA issuer (one lane; all lanes follow)
+        // ------------------------------------------------ MMA issuer (the elected lane; the warp stays together)
         bool ok = true;
         unsigned got = 0;                          // slots consumed
         unsigned n_p[2] = {0u, 0u}, n_o[2] = {0u, 0u};
+        const unsigned lead = elect_one();
         const unsigned idesc_s = instr_desc(CH_KEYS);
         const unsigned idesc_o = instr_desc(NDB * 64) | (1u << 16);          // right operand MN-major
         for (int k = 0; ok && work.next(it, r, c, tq, j.causal, j.max_new, j.few); ++k) {
@@ -385,19 +364,22 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 ok = __all_sync(0xffffffffu, ok);
             };
             auto issue_s = [&](int t, unsigned slot) {
-                const unsigned long long a = smem_desc_sw128(smem_u32(qs + t * NDB * BLK_BYTES));
-                const unsigned long long b = smem_desc_sw128(smem_u32(ring + (slot % SLOTS) * SLOT_BYTES));
-                umma_blocks<NDB>(tmem_base + t * 128, a, b, BLK_BYTES, BLK_BYTES, idesc_s);
-                umma_commit(&sh.s_full[t]);
+                const unsigned a = desc_lo(smem_u32(qs + t * NDB * BLK_BYTES));
+                const unsigned b = desc_lo(smem_u32(ring + (slot % SLOTS) * SLOT_BYTES));
+                
+#pragma unroll
+                for (int q = 0; q < NDB * 4; ++q)
+                    umma_ss(tmem_base + t * 128, a + (q >> 2) * (BLK_BYTES >> 4) + 2 * (q & 3), b + (q >> 2) * (BLK_BYTES >> 4) + 2 * (q & 3), idesc_s, q != 0, lead);
+                umma_commit_lead(&sh.s_full[t], lead);
             };
             wait_slot(got, 36);
             if (!ok) break;
             tcgen05_fence_after();
-            if (elect_one()) {
+            {
                 for (int t = 0; t < two; ++t)
                     if (nt[t] > 0) issue_s(t, got);
-                umma_commit(&sh.empty[got % SLOTS]);
-                if (it.take == 1) umma_commit(&sh.q_empty);
+                umma_commit_lead(&sh.empty[got % SLOTS], lead);
+                if (it.take == 1) umma_commit_lead(&sh.q_empty, lead);
             }
             for (int u = 0; u < it.take && ok; ++u, got += 2) {
                 const unsigned sv = got + 1, sk = got + 2;
@@ -421,31 +403,30 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     if (u >= nt[t]) continue;
                     // the accumulator is overwritten: the previous item's rows have been read out
                     if (u == 0 && n_o[t] > 0) ok = mbar_wait(&sh.o_empty[t], (n_o[t] - 1u) & 1u, abort_flag, 40);
-                    const unsigned long long b = smem_desc_mn(smem_u32(ring + (sv % SLOTS) * SLOT_BYTES));
+                    const unsigned b = desc_lo_mn(smem_u32(ring + (sv % SLOTS) * SLOT_BYTES), BLK_BYTES);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {                            // as soon as half of the probabilities are there
                         ok = ok && mbar_wait(&sh.p_full[t][h], n_p[t] & 1u, abort_flag, 39);
                         ok = __all_sync(0xffffffffu, ok);
                         if (!ok) break;
                         tcgen05_fence_after();
-                        if (elect_one())
 #pragma unroll
                             for (int q = 4 * h; q < 4 * h + 4; ++q)
-                                umma_ts(tmem_base + 256 + t * 128, tmem_base + t * 128 + q * 8, b + q * (2048 >> 4), idesc_o, (u | q) != 0);
+                                umma_ts(tmem_base + 256 + t * 128, tmem_base + t * 128 + q * 8, b + q * (2048 >> 4), idesc_o, (u | q) != 0, lead);
                     }
                     if (!ok) break;
                     ++n_p[t];
-                    if (elect_one()) {
+                    {
                         if (u + 1 < nt[t]) issue_s(t, sk);
-                        else umma_commit(&sh.o_full[t]);
+                        else umma_commit_lead(&sh.o_full[t], lead);
                     }
                     if (u + 1 >= nt[t]) ++n_o[t];
                 }
                 if (!ok) break;
-                if (elect_one()) {
-                    umma_commit(&sh.empty[sv % SLOTS]);
-                    if (ahead) umma_commit(&sh.empty[sk % SLOTS]);
-                    if (u + 2 == it.take) umma_commit(&sh.q_empty);   // the item's last scores are under way
+                {
+                    umma_commit_lead(&sh.empty[sv % SLOTS], lead);
+                    if (ahead) umma_commit_lead(&sh.empty[sk % SLOTS], lead);
+                    if (u + 2 == it.take) umma_commit_lead(&sh.q_empty, lead);   // the item's last scores are under way
                 }
             }
         }
@@ -473,29 +454,30 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 if (!ok) break;
                 ++n_s;
                 tcgen05_fence_after();
-                unsigned x[4][32];
+                unsigned x[2][32], z[2][32];
                 const int k0 = (it.ku + u) * CH_KEYS;
-                const bool masked = k0 + CH_KEYS > lim_tile;
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                auto most = [&](unsigned (&y)[32], int at) {                // (mask and) maximum of 32 scores
-                    if (masked) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (at + e >= lim) y[e] = 0xff800000u;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], y[e], y[e + 1]);
-                };
                 tmem_ld32_issue(t_s, x[0]);
                 tmem_ld32_issue(t_s + 32, x[1]);
-                tmem_ld_wait(x[0]); tmem_ld_wait(x[1]);
-                tmem_ld32_issue(t_s + 64, x[2]);
-                tmem_ld32_issue(t_s + 96, x[3]);
-                most(x[0], k0);
-                most(x[1], k0 + 32);
-                tmem_ld_wait(x[2]); tmem_ld_wait(x[3]);
-                most(x[2], k0 + 64);
-                most(x[3], k0 + 96);
+                tmem_ld32_issue(t_s + 64, z[0]);
+                tmem_ld32_issue(t_s + 96, z[1]);
+                tmem_ld_wait(x[0]); tmem_ld_wait(x[1]); tmem_ld_wait(z[0]); tmem_ld_wait(z[1]);
+                if (k0 + CH_KEYS > lim_tile) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            if (k0 + q * 32 + e >= lim) x[q][e] = 0xff800000u;
+                            if (k0 + 64 + q * 32 + e >= lim) z[q][e] = 0xff800000u;
+                        }
+                }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    mx[0] = max3(mx[0], x[0][e], x[0][e + 1]);
+                    mx[1] = max3(mx[1], x[1][e], x[1][e + 1]);
+                    mx[2] = max3(mx[2], z[0][e], z[0][e + 1]);
+                    mx[3] = max3(mx[3], z[1][e], z[1][e + 1]);
+                }
                 const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * j.scale);
                 if (u == 0) {
                     m = m_new;
@@ -518,18 +500,19 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     }
                 }
                 const float ref = m > -INFINITY ? m : 0.f;
-                float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
+                // (one copy of this code for both halves: with all of it unrolled a key tile's instructions no longer fit the
+                // instruction cache nearest to the scheduler)
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     unsigned w[32];
-                    if (masked) exp_pairs<true>(x[2 * h], x[2 * h + 1], j.scale, -ref, w, sum);
-                    else exp_pairs<false>(x[2 * h], x[2 * h + 1], j.scale, -ref, w, sum);
+                    exp_pairs(x[0], x[1], j.scale, -ref, w, l);
                     tmem_st32(t_s + h * 32, w);
                     tcgen05_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.p_full[t][h]);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) { x[0][e] = z[0][e]; x[1][e] = z[1][e]; }
                 }
-                l += sum.x + sum.y;
             }
             if (!ok) break;
             // ---- the item's rows
@@ -565,9 +548,10 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     }
                 }
             } else {
-                // a share of an item: unnormalised, columns x rows (a warp's lanes write next to each other)
+                // a share of an item: unnormalised, four columns of a row together (a warp's lanes write next to each other)
                 auto part = [&](int piece) { return ws + (2 * (int64_t)(it.c0 + piece) + (piece == 0 ? 1 : 0)) * PART_FLOATS; };
-                float* mine = part(it.piece) + t * 128 + i;
+                const int at = t * 128 + i;
+                float4* mine = reinterpret_cast<float4*>(part(it.piece)) + at;
 #pragma unroll
                 for (int q = 0; q < NDB * 2; ++q) {
                     unsigned y[32];
@@ -577,10 +561,12 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                         for (int e = 0; e < 32; ++e) y[e] = 0u;
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) __stcg(mine + (q * 32 + e) * 256, __uint_as_float(y[e]));
+                    for (int e = 0; e < 8; ++e)
+                        __stcg(mine + (q * 8 + e) * 256, make_float4(__uint_as_float(y[4 * e]), __uint_as_float(y[4 * e + 1]),
+                                                                     __uint_as_float(y[4 * e + 2]), __uint_as_float(y[4 * e + 3])));
                 }
-                __stcg(mine + 128 * 256, m);
-                __stcg(mine + 128 * 256 + 256, l);
+                __stcg(part(it.piece) + 128 * 256 + at, m);
+                __stcg(part(it.piece) + 128 * 256 + 256 + at, l);
                 __threadfence();
                 __syncwarp();
                 unsigned last = 0u;
@@ -593,12 +579,10 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 if (last) {
                     __threadfence();
                     float M = -INFINITY, L = 0.f;
-                    for (int p = 0; p < it.pieces; ++p) M = fmaxf(M, __ldcg(part(p) + t * 128 + i + 128 * 256));
+                    for (int p = 0; p < it.pieces; ++p) M = fmaxf(M, __ldcg(part(p) + 128 * 256 + at));
                     const float Mr = M > -INFINITY ? M : 0.f;
-                    for (int p = 0; p < it.pieces; ++p) {
-                        const float* o = part(p) + t * 128 + i + 128 * 256;
-                        L = fmaf(__ldcg(o + 256), ex2_approx(__ldcg(o) - Mr), L);
-                    }
+                    for (int p = 0; p < it.pieces; ++p)
+                        L = fmaf(__ldcg(part(p) + 128 * 256 + 256 + at), ex2_approx(__ldcg(part(p) + 128 * 256 + at) - Mr), L);
                     const float f = L > 0.f ? 1.0f / L : 0.f;
 #pragma unroll 1
                     for (int q = 0; q < NDB * 2; ++q) {                      // 32 columns of a piece in flight
@@ -608,13 +592,17 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                         for (int e = 0; e < 32; ++e) y[e] = 0.f;
 #pragma unroll 1
                         for (int p = 0; p < it.pieces; ++p) {
-                            const float* o = part(p) + t * 128 + i;
-                            const float fp = ex2_approx(__ldcg(o + 128 * 256) - Mr);
-                            float z[32];
+                            const float4* o = reinterpret_cast<const float4*>(part(p)) + q * 8 * 256 + at;
+                            const float mp = __ldcg(part(p) + 128 * 256 + at);
+                            float4 z[8];
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) z[e] = __ldcg(o + (q * 32 + e) * 256);
+                            for (int e = 0; e < 8; ++e) z[e] = __ldcg(o + e * 256);
+                            const float fp = ex2_approx(mp - Mr);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) y[e] = fmaf(z[e], fp, y[e]);
+                            for (int e = 0; e < 8; ++e) {
+                                y[4 * e] = fmaf(z[e].x, fp, y[4 * e]); y[4 * e + 1] = fmaf(z[e].y, fp, y[4 * e + 1]);
+                                y[4 * e + 2] = fmaf(z[e].z, fp, y[4 * e + 2]); y[4 * e + 3] = fmaf(z[e].w, fp, y[4 * e + 3]);
+                            }
                         }
                         if (live) {
 #pragma unroll

@@ -19,12 +19,49 @@ static __device__ __forceinline__ void tma_load_4d(const CUtensorMap* map, unsig
 
 // One lane of a converged warp, the same one every time.  The compiler knows that it is one: operands of MMAs and TMA loads,
 // which are uniform registers, are then moved there once, and not lane by lane as behind a comparison with the lane's
-// number (eight MMAs of 128 x 128 x 16: 640 -> 490 cycles to issue; they execute in 512).
+// number.
 static __device__ __forceinline__ bool elect_one() {
     unsigned p;
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
     return p != 0u;
 }
+// MMAs of a converged warp, executed by the lane whose `lead` is not 0 (elect_one): without a branch around them, and with
+// descriptors as their low words (address and leading offset; the high word, SBO 1024, version 1, 128-byte swizzle, is a
+// constant), an instruction takes 68 cycles to issue beside two busy warps on its scheduler, where the tensor core takes 64;
+// behind `if (elect_one())` 78, behind `if (lane == 0)` 168.
+static constexpr unsigned DESC_HI = 0x40004040u;
+static __device__ __forceinline__ void umma_ss(unsigned tmem_d, unsigned a_lo, unsigned b_lo, unsigned idesc,
+                                               unsigned accumulate, unsigned lead) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 x, y;\n\t"
+        "mov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %6, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(DESC_HI), "r"(lead)
+        : "memory");
+}
+// left operand in TMEM
+static __device__ __forceinline__ void umma_ts(unsigned tmem_d, unsigned tmem_a, unsigned b_lo, unsigned idesc,
+                                               unsigned accumulate, unsigned lead) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t.reg .b64 y;\n\t"
+        "mov.b64 y, {%2, %5};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %6, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(DESC_HI), "r"(lead)
+        : "memory");
+}
+static __device__ __forceinline__ void umma_commit_lead(unsigned long long* bar, unsigned lead) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %1, 0;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+        ::"r"(smem_u32(bar)), "r"(lead)
+        : "memory");
+}
+// low descriptor words of a K-major tile (rows of 128 bytes) and of an MN-major one (128-byte rows of 64 elements, the
+// next 64 elements `next` bytes further on)
+static __device__ __forceinline__ unsigned desc_lo(unsigned addr) { return (addr >> 4) | 0x10000u; }
+static __device__ __forceinline__ unsigned desc_lo_mn(unsigned addr, unsigned next) { return (addr >> 4) | ((next >> 4) << 16); }
 
 static __device__ __forceinline__ float ex2_approx(float x) {
     float y;
