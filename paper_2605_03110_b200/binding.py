@@ -436,6 +436,7 @@ class KVCache:
         if any(t is not None and t.device != K.device for t in (V, table, kmin, kmax)):
             raise ValueError("the cache's tensors must be on one device")
         self.K, self.V, self.table, self.kmin, self.kmax = K, V, table, kmin, kmax
+        self.K_dtype = K.dtype
         self.dtype, self.h_kv, self.d_h, self.page_size, self.B = dtype, h_kv, d, ps, table.shape[0]
         self._c = _KVCacheStruct(K.data_ptr(), V.data_ptr(), _ptr(kmin), _ptr(kmax), table.data_ptr(),
                                  max(table.stride(0), table.shape[1]), table.shape[1], n,
@@ -444,7 +445,7 @@ class KVCache:
 
 
 def _int32(t: torch.Tensor, name: str, n: Optional[int] = None) -> None:
-    if t.dtype != torch.int32:
+    if t.dtype is not torch.int32:
         raise TypeError(f"{name} must be int32")
     if n is not None and (t.numel() < n or not t.is_contiguous()):
         raise ValueError(f"{name} must be dense with at least {n} entries")
@@ -460,15 +461,16 @@ def _ragged(cache: KVCache, off: torch.Tensor, length: torch.Tensor) -> int:
     return B
 
 
-def _rows_of(X: torch.Tensor, name: str, cache: KVCache, N: Optional[int] = None):
+def _rows_of(X: torch.Tensor, name: str, cache: KVCache, N: Optional[int] = None, heads: Optional[int] = None):
     """(N, heads, row stride) of per-token rows (N, heads, d_h), heads side by side."""
-    if X.dim() != 3 or X.shape[2] != cache.d_h or N is not None and X.shape[0] != N:
-        raise ValueError(f"{name} must be N x heads x d_h")
-    if X.dtype != cache.K.dtype:
+    shape, strides, d = X.shape, X.stride(), cache.d_h      # (each once: a call's checks are on the way of every token)
+    if len(shape) != 3 or shape[2] != d or N is not None and shape[0] != N or heads is not None and shape[1] != heads:
+        raise ValueError(f"{name} must be {'N' if N is None else N} x {'heads' if heads is None else heads} x d_h")
+    if X.dtype is not cache.K_dtype:
         raise TypeError(f"{name} must have the cache's type")
-    if X.stride(2) != 1 or X.shape[1] > 1 and X.stride(1) != X.shape[2]:
+    if strides[2] != 1 or strides[1] != d and shape[1] > 1:
         raise ValueError(f"{name} must hold the heads of a token side by side")
-    return X.shape[0], X.shape[1], X.stride(0) if X.shape[0] > 1 else X.shape[1] * X.shape[2]
+    return shape[0], shape[1], strides[0] if shape[0] > 1 else shape[1] * d
 
 
 def ada_cache_append(ctx: Context, cache: KVCache, K: torch.Tensor, V: torch.Tensor, off: torch.Tensor,
@@ -482,24 +484,23 @@ def ada_cache_append(ctx: Context, cache: KVCache, K: torch.Tensor, V: torch.Ten
     have; sequence b has rows off[b] .. off[b + 1].  Q (N, h, d_h) is normed and rotated alongside.  rep_idx, rep_cnt:
     only these tokens are kept (the lists of a selection call).  Returns (q_out or None, len_out)."""
     B = _ragged(cache, off, length)
-    N, hk, ldk = _rows_of(K, "K", cache)
-    _, hv, ldv = _rows_of(V, "V", cache, N)
-    if hk != cache.h_kv or hv != cache.h_kv:
-        raise ValueError("K and V must have the cache's heads")
+    N, _, ldk = _rows_of(K, "K", cache, None, cache.h_kv)
+    _, _, ldv = _rows_of(V, "V", cache, N, cache.h_kv)
     if len_out is None:
         len_out = torch.empty(B, dtype=torch.int32, device=K.device)
-    _int32(len_out, "len_out", B)
+    else:
+        _int32(len_out, "len_out", B)
     h = ldq = ldqo = 0
     if Q is not None:
         _, h, ldq = _rows_of(Q, "Q", cache, N)
         if q_out is None:
             q_out = torch.empty((N, h, cache.d_h), dtype=Q.dtype, device=Q.device)
-        _, ho, ldqo = _rows_of(q_out, "q_out", cache, N)
-        if ho != h:
-            raise ValueError("q_out must have Q's heads")
+            ldqo = h * cache.d_h
+        else:
+            _, _, ldqo = _rows_of(q_out, "q_out", cache, N, h)
     for w in (q_norm, k_norm):
         if w is not None:
-            if w.dtype != K.dtype:
+            if w.dtype is not cache.K_dtype:
                 raise TypeError("the norms' weights must have the cache's type")
             if w.shape != (cache.d_h,) or not w.is_contiguous():
                 raise ValueError("the norms' weights must be d_h dense elements")
@@ -529,9 +530,7 @@ def ada_attention_cached(ctx: Context, cache: KVCache, Q: torch.Tensor, off: tor
     N, h, ldq = _rows_of(Q, "Q", cache)
     if out is None:
         out = torch.zeros((N, h, cache.d_h), dtype=Q.dtype, device=Q.device)
-    _, ho, ldo = _rows_of(out, "out", cache, N)
-    if ho != h:
-        raise ValueError("out must have Q's heads")
+    _, _, ldo = _rows_of(out, "out", cache, N, h)
     st = _fast.attention_cached(ctx.addr, cache.addr, B, off, length, N, max_new, Q, h, ldq, cache.dtype, scale, out, ldo,
                                 flags, _stream_of(ctx, stream))
     if st:
@@ -540,11 +539,12 @@ def ada_attention_cached(ctx: Context, cache: KVCache, Q: torch.Tensor, off: tor
 
 
 def _lists_of(cache: KVCache, N: int, blk_idx: torch.Tensor, blk_cnt: torch.Tensor, k: Optional[int] = None) -> int:
-    if blk_idx.dim() != 3 or blk_idx.shape[:2] != (N, cache.h_kv) or k is not None and blk_idx.shape[2] != k:
+    shape = blk_idx.shape
+    if len(shape) != 3 or shape[0] != N or shape[1] != cache.h_kv or k is not None and shape[2] != k:
         raise ValueError("blk_idx must be N x h_kv x k")
-    _int32(blk_idx, "blk_idx", blk_idx.numel())
+    _int32(blk_idx, "blk_idx", N * cache.h_kv * shape[2])
     _int32(blk_cnt, "blk_cnt", N * cache.h_kv)
-    return blk_idx.shape[2]
+    return shape[2]
 
 
 def ada_select_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: torch.Tensor, length: torch.Tensor, k: int,
@@ -554,11 +554,13 @@ def ada_select_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: torch.
     blk_cnt int32 (N, h_kv)); rows behind the last sequence are left as they are."""
     B = _ragged(cache, off, length)
     N, h, ldq = _rows_of(Q, "Q", cache)
-    if blk_idx is None:
+    if blk_idx is None and blk_cnt is None:
         blk_idx = torch.empty((N, cache.h_kv, k), dtype=torch.int32, device=Q.device)
-    if blk_cnt is None:
         blk_cnt = torch.empty((N, cache.h_kv), dtype=torch.int32, device=Q.device)
-    _lists_of(cache, N, blk_idx, blk_cnt, k)
+    elif blk_idx is None or blk_cnt is None:
+        raise ValueError("blk_idx and blk_cnt are given together")
+    else:
+        _lists_of(cache, N, blk_idx, blk_cnt, k)
     st = _fast.select_blocks(ctx.addr, cache.addr, B, off, length, N, Q, h, ldq, cache.dtype, k, n_first, n_last, blk_idx,
                              blk_cnt, flags, _stream_of(ctx, stream))
     if st:
@@ -575,9 +577,7 @@ def ada_attention_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: tor
     k = _lists_of(cache, N, blk_idx, blk_cnt)
     if out is None:
         out = torch.zeros((N, h, cache.d_h), dtype=Q.dtype, device=Q.device)
-    _, ho, ldo = _rows_of(out, "out", cache, N)
-    if ho != h:
-        raise ValueError("out must have Q's heads")
+    _, _, ldo = _rows_of(out, "out", cache, N, h)
     st = _fast.attention_blocks(ctx.addr, cache.addr, B, off, length, N, Q, h, ldq, cache.dtype, blk_idx, blk_cnt, k, scale,
                                 out, ldo, flags, _stream_of(ctx, stream))
     if st:

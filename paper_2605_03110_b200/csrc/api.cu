@@ -192,6 +192,7 @@ ada_status ada_create(ada_ctx** out, int device, int64_t maxB, int64_t maxT, int
     ctx->host_event = nullptr; ctx->host_ready = nullptr; ctx->host_out = false;
     ctx->attn_ws = nullptr; ctx->attn_ws_bytes = 0;
     ctx->cache_ws = nullptr; ctx->cache_part = nullptr; ctx->cache_ctr = nullptr; ctx->cache_ctr_bytes = 0;
+    ctx->cache_attr = 0;
     ctx->map_cache = nullptr;
     ctx->tc_attr_set = false;
     ctx->cooperative = true;

@@ -11,6 +11,11 @@
 // heads), half a warp (d_h <= 64: a quarter) one head's row at a time.  A lane holds two pieces of four elements that the
 // rotation pairs with each other, so that it needs nobody else's elements, and keeps the four sines and cosines of
 // its pairs, and the norm's weights, in registers for all heads of the token.
+//
+// The bounds of a page need all of its keys.  Calls of several tokens each form them in a second kernel, from the pages.  Where
+// there are no more tokens than sequences (a decoding step) the second launch would take as long as the first: there a
+// warp of its own takes each key head of a token and reads the page's older keys beside the new one; should several new
+// tokens lie in a page, the last one's warp forms the others' keys once more.
 #include "cache_dev.cuh"
 
 namespace ada {
@@ -53,6 +58,39 @@ __device__ __forceinline__ void angles(const AppendJob& j, const Lane& ln, int v
     }
 }
 
+// A head's row in a lane's registers, normed (g: the lane's weights) and rotated
+template <int LG, bool PAIRS>
+__device__ __forceinline__ void transform(uint2& a, uint2& b, bool norm, const float (&g)[8], float eps, int d, const float (&cs)[4],
+                                          const float (&sn)[4], unsigned mask) {
+    float x[8];
+    unpack4(a, x);
+    unpack4(b, x + 4);
+    if (norm) {
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
+#pragma unroll
+        for (int m = LG / 2; m > 0; m >>= 1) s += __shfl_xor_sync(mask, s, m, LG);
+        const float f = rsqrtf(s / (float)d + eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= f * g[e];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                                // (an unrotated lane has cosine 1, sine 0)
+        const int p = PAIRS ? 2 * i : i, q = PAIRS ? 2 * i + 1 : 4 + i;
+        const float y = x[p], z = x[q];
+        x[p] = y * cs[i] - z * sn[i];
+        x[q] = z * cs[i] + y * sn[i];
+    }
+    a = pack4(x);
+    b = pack4(x + 4);
+}
+__device__ __forceinline__ void weights(const __nv_bfloat16* w, const Lane& ln, float (&g)[8]) {
+    if (w == nullptr) return;
+    unpack4(ln.on ? *reinterpret_cast<const uint2*>(w + ln.e0) : make_uint2(0u, 0u), g);
+    unpack4(ln.on ? *reinterpret_cast<const uint2*>(w + ln.e1) : make_uint2(0u, 0u), g + 4);
+}
+
 // Rows first, first + step, .. < count of one token, `src` to `dst`, head x at x * d (src) and x * dst_step (dst):
 // normed by the lane's weights w (NULL: not), rotated.
 template <int LG, bool PAIRS>
@@ -60,10 +98,7 @@ __device__ __forceinline__ void move_rows(const __nv_bfloat16* src, __nv_bfloat1
                                           int count, int d, const Lane& ln, const __nv_bfloat16* w, float eps, bool rotate,
                                           const float (&cs)[4], const float (&sn)[4], unsigned mask, bool& bad) {
     float g[8];
-    if (w != nullptr) {
-        unpack4(ln.on ? *reinterpret_cast<const uint2*>(w + ln.e0) : make_uint2(0u, 0u), g);
-        unpack4(ln.on ? *reinterpret_cast<const uint2*>(w + ln.e1) : make_uint2(0u, 0u), g + 4);
-    }
+    weights(w, ln, g);
     for (int x0 = first; x0 < count; x0 += APP_ROWS * step) {
         uint2 a[APP_ROWS], b[APP_ROWS];
 #pragma unroll
@@ -79,30 +114,7 @@ __device__ __forceinline__ void move_rows(const __nv_bfloat16* src, __nv_bfloat1
         for (int u = 0; u < APP_ROWS; ++u) {
             if (x0 + u * step >= count) break;                   // (the same for all lanes of the group)
             bad = bad || nonfinite4(a[u]) || nonfinite4(b[u]);
-            if (w != nullptr || rotate) {
-                float x[8];
-                unpack4(a[u], x);
-                unpack4(b[u], x + 4);
-                if (w != nullptr) {
-                    float s = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
-#pragma unroll
-                    for (int m = LG / 2; m > 0; m >>= 1) s += __shfl_xor_sync(mask, s, m, LG);
-                    const float f = rsqrtf(s / (float)d + eps);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] *= f * g[e];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {                    // (an unrotated lane has cosine 1, sine 0)
-                    const int p = PAIRS ? 2 * i : i, q = PAIRS ? 2 * i + 1 : 4 + i;
-                    const float y = x[p], z = x[q];
-                    x[p] = y * cs[i] - z * sn[i];
-                    x[q] = z * cs[i] + y * sn[i];
-                }
-                a[u] = pack4(x);
-                b[u] = pack4(x + 4);
-            }
+            if (w != nullptr || rotate) transform<LG, PAIRS>(a[u], b[u], w != nullptr, g, eps, d, cs, sn, mask);
             if (ln.on) {
                 __nv_bfloat16* p = dst + (x0 + u * step) * dst_step;
                 *reinterpret_cast<uint2*>(p + ln.e0) = a[u];
@@ -112,15 +124,24 @@ __device__ __forceinline__ void move_rows(const __nv_bfloat16* src, __nv_bfloat1
     }
 }
 
-// A warp: one token, or one of `shares` parts of its heads.  LG lanes have a head's row.
-template <int LG, bool PAIRS>
+__device__ __forceinline__ void widen(uint2& lo, uint2& hi, const uint2& a, const uint2& b) {
+    __nv_bfloat162 *l = reinterpret_cast<__nv_bfloat162*>(&lo), *h = reinterpret_cast<__nv_bfloat162*>(&hi);
+    const __nv_bfloat162 *x = reinterpret_cast<const __nv_bfloat162*>(&a), *y = reinterpret_cast<const __nv_bfloat162*>(&b);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) { l[i] = __hmin2(l[i], x[i]); h[i] = __hmax2(h[i], y[i]); }
+}
+
+// A warp: one token, or one of `shares` parts of its heads.  LG lanes have a head's row.  STEP: after the queries' shares every
+// key head of the token has a warp of its own, which also forms the page's bounds.
+template <int LG, bool PAIRS, bool STEP>
 __global__ void __launch_bounds__(APP_THREADS)
 k_cache_append(const CacheView c, const Ragged r, const AppendJob j, int shares, unsigned* __restrict__ status) {
     grid_dep_wait();
     grid_dep_launch_next();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int item = blockIdx.x * APP_WARPS + warp;
-    const int i = item / shares, share = item - i * shares;
+    const int parts = STEP ? shares + c.h_kv : shares;
+    const int i = item / parts, share = item - i * parts;
     if (blockIdx.x == 0) {
         check_ragged(r, c, status, threadIdx.x, APP_THREADS);
         if (j.len_out != nullptr)
@@ -174,10 +195,79 @@ k_cache_append(const CacheView c, const Ragged r, const AppendJob j, int shares,
     float cs[4], sn[4];
     angles(j, ln, v, p0 + li, cs, sn);
     bool bad = false;
-    if (j.Q != nullptr)
+    if (j.Q != nullptr && (!STEP || share < shares))
         move_rows<LG, PAIRS>(j.Q + (int64_t)i * j.ldq, j.q_out + (int64_t)i * j.ldqo, c.d, first, step, j.h, c.d, ln, j.q_norm,
                              j.eps, rotate, cs, sn, mask, bad);
-    if (page >= 0) {
+    if (STEP) {
+        const int head = share - shares;
+        if (head >= 0 && page >= 0) {
+            const unsigned full = 0xffffffffu;
+            const int64_t at0 = slot_at(c, page, head, 0);
+            const bool own = lane < LG;                          // (one group of lanes writes)
+            // the page's slots [0, s0) are older, [s0, slot] come from this call
+            const bool last = c.kmin != nullptr && (li + 1 == kept || slot == (1 << c.shift) - 1);
+            const int s0 = max(slot - li, 0);
+            uint2 lo[2], hi[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) { lo[u] = make_uint2(0x7f807f80u, 0x7f807f80u); hi[u] = make_uint2(0xff80ff80u, 0xff80ff80u); }
+            float g[8];
+            weights(j.k_norm, ln, g);
+            int turned = li;                                     // whose angles the lane has
+            for (int t = last ? li - (slot - s0) : li; t <= li; ++t) {      // this token, or all new ones of the page
+                const int tok = j.rep_idx != nullptr ? min(max(j.rep_idx[o + t], 0), n - 1) : t;
+                if (tok != turned) angles(j, ln, v, p0 + tok, cs, sn);
+                turned = tok;
+                uint2 a = make_uint2(0u, 0u), b2 = a;
+                if (ln.on) {
+                    const __nv_bfloat16* p = j.K + (int64_t)(o + tok) * j.ldk + (int64_t)head * c.d;
+                    a = *reinterpret_cast<const uint2*>(p + ln.e0);
+                    b2 = *reinterpret_cast<const uint2*>(p + ln.e1);
+                }
+                if (t == li) bad = bad || nonfinite4(a) || nonfinite4(b2);
+                if (j.k_norm != nullptr || rotate) transform<LG, PAIRS>(a, b2, j.k_norm != nullptr, g, j.eps, c.d, cs, sn, mask);
+                if (t == li && own && ln.on) {
+                    *reinterpret_cast<uint2*>(c.k + at0 + (int64_t)slot * c.d + ln.e0) = a;
+                    *reinterpret_cast<uint2*>(c.k + at0 + (int64_t)slot * c.d + ln.e1) = b2;
+                }
+                widen(lo[0], hi[0], a, a);
+                widen(lo[1], hi[1], b2, b2);
+            }
+            if (own && ln.on) {
+                const __nv_bfloat16* p = j.V + (int64_t)(o + at) * j.ldv + (int64_t)head * c.d;
+                const uint2 a = *reinterpret_cast<const uint2*>(p + ln.e0), b2 = *reinterpret_cast<const uint2*>(p + ln.e1);
+                bad = bad || nonfinite4(a) || nonfinite4(b2);
+                *reinterpret_cast<uint2*>(c.v + at0 + (int64_t)slot * c.d + ln.e0) = a;
+                *reinterpret_cast<uint2*>(c.v + at0 + (int64_t)slot * c.d + ln.e1) = b2;
+            }
+            if (last) {
+                if (ln.on) {                                     // the groups of lanes take turns at the older keys
+                    const __nv_bfloat16* p = c.k + at0;
+#pragma unroll 8
+                    for (int q = lane / LG; q < s0; q += PER) {
+                        const uint2 a = *reinterpret_cast<const uint2*>(p + (int64_t)q * c.d + ln.e0);
+                        const uint2 b2 = *reinterpret_cast<const uint2*>(p + (int64_t)q * c.d + ln.e1);
+                        widen(lo[0], hi[0], a, a);
+                        widen(lo[1], hi[1], b2, b2);
+                    }
+                }
+#pragma unroll
+                for (int m = LG; m < 32; m <<= 1)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint2 a = make_uint2(__shfl_xor_sync(full, lo[u].x, m), __shfl_xor_sync(full, lo[u].y, m));
+                        const uint2 b2 = make_uint2(__shfl_xor_sync(full, hi[u].x, m), __shfl_xor_sync(full, hi[u].y, m));
+                        widen(lo[u], hi[u], a, b2);
+                    }
+                if (own && ln.on) {
+                    const int64_t to = ((int64_t)page * c.h_kv + head) * c.d;
+                    *reinterpret_cast<uint2*>(c.kmin + to + ln.e0) = lo[0];
+                    *reinterpret_cast<uint2*>(c.kmin + to + ln.e1) = lo[1];
+                    *reinterpret_cast<uint2*>(c.kmax + to + ln.e0) = hi[0];
+                    *reinterpret_cast<uint2*>(c.kmax + to + ln.e1) = hi[1];
+                }
+            }
+        }
+    } else if (page >= 0) {
         const int64_t at0 = slot_at(c, page, 0, slot), head_step = (int64_t)c.d << c.shift;
         if (at != li) angles(j, ln, v, p0 + at, cs, sn);
         move_rows<LG, PAIRS>(j.K + (int64_t)(o + at) * j.ldk, c.k + at0, head_step, first, step, c.h_kv, c.d, ln, j.k_norm, j.eps,
@@ -260,16 +350,20 @@ k_cache_bounds(const CacheView c, const Ragged r, const int32_t* __restrict__ re
 cudaError_t launch_cache_append(ada_ctx* ctx, const CacheView& c, const Ragged& r, const AppendJob& j, cudaStream_t s) {
     // a token's heads are dealt to several warps while the tokens alone do not fill the GPU: as many as leave a warp
     // one round of rows of the larger of queries and keys
-    const int per = c.d <= 64 ? 4 : 2, heads = j.h > c.h_kv ? j.h : c.h_kv;
+    const int per = c.d <= 64 ? 4 : 2;
+    const bool step = r.N <= r.B && (int64_t)r.N * (c.h_kv + j.h) < (int64_t)1 << 30;
+    const int heads = step ? j.h : j.h > c.h_kv ? j.h : c.h_kv;
     const int want = (heads + per * APP_ROWS - 1) / (per * APP_ROWS), room = 16 * ctx->sm_count / r.N;
-    const int shares = room < 1 ? 1 : want < room ? want : room;
-    const int64_t items = (int64_t)r.N * shares;
-    auto kernel = c.d <= 64 ? (j.pairs ? k_cache_append<8, true> : k_cache_append<8, false>)
-                            : (j.pairs ? k_cache_append<16, true> : k_cache_append<16, false>);
+    const int shares = room < 1 ? (heads > 0 ? 1 : 0) : want < room ? want : room;
+    const int64_t items = (int64_t)r.N * (step ? shares + c.h_kv : shares);
+    auto kernel = step ? (c.d <= 64 ? (j.pairs ? k_cache_append<8, true, true> : k_cache_append<8, false, true>)
+                                    : (j.pairs ? k_cache_append<16, true, true> : k_cache_append<16, false, true>))
+                       : (c.d <= 64 ? (j.pairs ? k_cache_append<8, true, false> : k_cache_append<8, false, false>)
+                                    : (j.pairs ? k_cache_append<16, true, false> : k_cache_append<16, false, false>));
     cudaError_t e = launch_k(ctx, kernel, dim3((unsigned)((items + APP_WARPS - 1) / APP_WARPS)), dim3(APP_THREADS), 0, s, c, r, j,
                              shares, ctx->status);
     if (e != cudaSuccess) return e;
-    if (c.kmin != nullptr) {
+    if (c.kmin != nullptr && !step) {
         // a sequence of n new tokens writes to at most n and at most (n - 1) / ps + 2 pages
         const int64_t most = (int64_t)(r.N >> c.shift) + 2 * (int64_t)r.B;
         const int pages = (int)(most < r.N ? most : r.N);

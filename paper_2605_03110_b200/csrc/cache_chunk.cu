@@ -653,7 +653,7 @@ bool encode_queries(CUtensorMap* map, const CacheView& c, const Ragged& r, const
 template <int NDB>
 cudaError_t run_chunk(ada_ctx* ctx, const ChunkMaps& maps, const CacheView& c, const Ragged& r, const AttendJob& j, int tq,
                       cudaStream_t s) {
-    cudaError_t e = cudaFuncSetAttribute(k_cache_chunk<NDB>, cudaFuncAttributeMaxDynamicSharedMemorySize, ch_smem<NDB>());
+    cudaError_t e = allow_smem(ctx, 11 + NDB, k_cache_chunk<NDB>, ch_smem<NDB>());                // bits 12, 13
     if (e != cudaSuccess) return e;
     return launch_k(ctx, k_cache_chunk<NDB>, dim3(ctx->sm_count), dim3(CH_THREADS), ch_smem<NDB>(), s, maps, c, r, j, tq,
                     ctx->cache_part, ctx->cache_ctr, ctx->status);

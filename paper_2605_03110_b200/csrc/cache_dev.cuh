@@ -38,9 +38,11 @@ static __device__ __forceinline__ int seq_len(const Ragged& r, const CacheView& 
     return min(max(r.len[b], 0), c.max_pages << c.shift);
 }
 // The sequence of row i, by all lanes of a warp together: the last b with off[b] <= i.  -1 if the row is no
-// sequence's (behind the last one, or the offsets are out of order).
+// sequence's (behind the last one, or the offsets are out of order).  A call with no more rows than sequences is mostly
+// one token each: looked at first, it saves two dependent loads.
 static __device__ __forceinline__ int seq_of_row(const Ragged& r, int i) {
     const int lane = threadIdx.x & 31;
+    if (r.N <= r.B && r.off[i] == i && r.off[i + 1] == i + 1) return i;
     int lo = 0, n = r.B;                         // the answer, if any, is in [lo, lo + n)
     while (n > 1) {
         const int step = (n + 31) >> 5, at = lane * step;
@@ -78,6 +80,15 @@ static __device__ __forceinline__ int64_t slot_at(const CacheView& c, int page, 
     return (int64_t)page * c.page_stride + ((int64_t)(head << c.shift) + slot) * c.d;
 }
 #endif
+
+// Dynamic shared memory above 48 KB has to be allowed for a kernel, once per device: `bit` says which kernel it is.
+template <typename K>
+inline cudaError_t allow_smem(ada_ctx* ctx, int bit, K kernel, int bytes) {
+    if (ctx->cache_attr >> bit & 1u) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) ctx->cache_attr |= 1u << bit;
+    return e;
+}
 
 // launchers -------------------------------------------------------------------------------------
 struct AppendJob {

@@ -486,7 +486,7 @@ cudaError_t launch_cache_select(ada_ctx* ctx, const CacheView& c, const Ragged& 
     const int keys = c.max_pages * 8, stages = 2 * sel_stage(c.d);
     const int room = ((keys > stages ? keys : stages) + 15) / 16 * 16;
     const int smem = room + 4 * SEL_ROWS * sel_row(c.d) + rows * stride * 4;
-    cudaError_t e = cudaFuncSetAttribute(k_cache_select, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024 - (int)sizeof(SelShared));
+    cudaError_t e = allow_smem(ctx, 14, k_cache_select, 226 * 1024 - (int)sizeof(SelShared));
     if (e != cudaSuccess) return e;
     return launch_k(ctx, k_cache_select, dim3(r.N / rows + (rows > 1 ? (r.B < r.N ? r.B : r.N) : 0), c.h_kv), dim3(SEL_THREADS), smem, s, c, r, j, rows,
                     stride, room, ctx->status);

@@ -213,6 +213,7 @@ struct ada_ctx {
     float* cache_part;
     unsigned* cache_ctr;
     size_t cache_ctr_bytes;
+    unsigned cache_attr;         // its kernels that are configured, by bit (one device: the context's)
     void* map_cache;     // tc::MapCache, or NULL: none kept
     // staging for the *_host entry points (allocated on first use)
     char* stage;

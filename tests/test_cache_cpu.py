@@ -176,9 +176,10 @@ def test_call_tensors(ada):
             (lambda: attend(Q[..., :32], off, n, 4), ValueError), (lambda: attend(Q[:, :, ::2], off, n, 4), ValueError),
             (lambda: attend(Q[:, ::2], off, n, 4), ValueError), (lambda: attend(Q[0], off, n, 4), ValueError),
             (lambda: attend(Q, off, n, 4, out=Q.float()), TypeError), (lambda: attend(Q, off, n, 4, out=K), ValueError),
-            (lambda: select(Q, off, n, 4, blk_idx=idx[:, :, :3]), ValueError),
-            (lambda: select(Q, off, n, 4, blk_idx=idx.long()), TypeError),
-            (lambda: select(Q, off, n, 4, blk_cnt=cnt[:3]), ValueError),
+            (lambda: select(Q, off, n, 4, blk_idx=idx[:, :, :3], blk_cnt=cnt), ValueError),
+            (lambda: select(Q, off, n, 4, blk_idx=idx.long(), blk_cnt=cnt), TypeError),
+            (lambda: select(Q, off, n, 4, blk_idx=idx, blk_cnt=cnt[:3]), ValueError),
+            (lambda: select(Q, off, n, 4, blk_cnt=cnt), ValueError),
             (lambda: blocks(Q, off, n, idx[:6], cnt), ValueError), (lambda: blocks(Q, off, n, idx[:, :1], cnt), ValueError),
             (lambda: blocks(Q, off, n, idx, cnt.float()), TypeError),
             (lambda: append(Q, K, off, n), ValueError), (lambda: append(K, K[:3], off, n), ValueError),

@@ -331,9 +331,12 @@ def near(got, want, row_max):
                                                    (5, 5, 96, 0, False, False), (2, 1, 128, 64, False, False)])
 def test_append(ada, ctx, h, hk, d, rot, pairs, norm, ps):
     g = torch.Generator().manual_seed(d + rot)
-    for news, olds in (([1, 1, 1], [0, 15, 200]), ([70, 0, 33], [5, 9, 64]), ([700], [0])):
+    # (no more rows than sequences: the form for single tokens, also where they are not spread one to each)
+    for news, olds, pad in (([1, 1, 1], [0, 15, 200], 3), ([70, 0, 33], [5, 9, 64], 3), ([700], [0], 3),
+                            ([1, 1, 1, 1], [0, 15, 16, 200], 0), ([5, 0, 0, 1, 0, 0, 0, 0], [14, 3, 0, 31, 1, 2, 3, 4], 2),
+                            ([0] * 30 + [20] + [0] * 10, [5] * 41, 21)):
         lens = [a + b for a, b in zip(news, olds)]
-        c = Case(ada, 40, h, hk, d, ps, news, lens, pad=3, planes=True)
+        c = Case(ada, 40, h, hk, d, ps, news, lens, pad=pad, planes=True)
         qkv = torch.randn((c.N, (h + 2 * hk) * d), generator=g).bfloat16()
         qkv[c.off[-1]:] = math.nan                       # padding is not read
         Q, K, V = (x.unflatten(1, (-1, d)) for x in qkv.split([h * d, hk * d, hk * d], 1))
@@ -401,6 +404,29 @@ def test_append_of_representatives(ada, ctx):
     assert near(c.cache.K.cpu().nan_to_num(), want[0].nan_to_num(), 8.0)
     assert torch.equal(c.cache.V.cpu().nan_to_num(), want[1].nan_to_num())
     assert near(c.cache.kmax.cpu().nan_to_num(), want[3].nan_to_num(), 8.0)
+
+
+def test_append_of_representatives_to_few_rows(ada, ctx):
+    """The form for single tokens with lists: kept tokens that share a page."""
+    news, olds = [6, 0, 0, 1, 0, 0, 0], [14, 2, 0, 3, 1, 1, 1]
+    lists = [[0, 2, 3, 5], [], [], [0], [], [], []]
+    lens = [o + len(x) for o, x in zip(olds, lists)]
+    c = Case(ada, 44, 4, 2, 64, 16, news, [max(x, 1) for x in lens])
+    g = torch.Generator().manual_seed(2)
+    K, V = (torch.randn((c.N, 2, 64), generator=g).bfloat16() for _ in range(2))
+    f = 10000.0 ** (-torch.arange(0, 64, 2, dtype=torch.float64) / 64)
+    idx = torch.full((c.N,), -1, dtype=torch.int32)
+    for b, x in enumerate(lists):
+        idx[c.off[b]:c.off[b] + len(x)] = torch.tensor(x, dtype=torch.int32)
+    pos0 = [100 * b for b in range(7)]
+    want = ref.append(c.cpu, K, V, c.off, olds, c.Q, None, None, 1e-6, f, False, pos0, lists)
+    q, n = ada.ada_cache_append(ctx, c.cache, K.cuda(), V.cuda(), c.d_off, i32(olds), Q=c.d_Q, inv_freq=f.cuda(),
+                                pos0=i32(pos0), rep_idx=idx.cuda(), rep_cnt=i32([len(x) for x in lists]))
+    fine(ada, ctx)
+    assert n.tolist() == lens and near(q, want[4], 8.0)
+    for got, w in ((c.cache.K, want[0]), (c.cache.kmin, want[2]), (c.cache.kmax, want[3])):
+        assert near(got.cpu().nan_to_num(), w.nan_to_num(), 8.0)
+    assert torch.equal(c.cache.V.cpu().nan_to_num(), want[1].nan_to_num())
 
 
 def test_bounds_of_a_page_that_was_taken_back(ada, ctx):
