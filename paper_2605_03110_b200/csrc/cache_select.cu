@@ -6,13 +6,15 @@
 //   s(p) = sum_e P_e kmax_pe + M_e kmin_pe:
 // one dot product of 2 d_h elements, whatever the number of heads.
 //
-// The choice is that of scores in 64 bits, but few of them are ever formed.  A block scores 16 tokens of a sequence
-// against all pages on mma.sync: P and M as two bf16 terms each, products exact, fp32 sums.  What that leaves out is
-// bounded (E below), so a page whose approximate score is more than 2 E above (below) the k-th largest is
-// certainly in (out); the few in between are scored again in 64 bits by the warp that has the row.  Rows with more such
-// pages than lanes (equal scores, infinities) are done in 64 bits throughout, by the whole block.
+// The choice is that of scores in 64 bits, but few of them are ever formed.  fp32 scores whose error is bounded (E below)
+// come first: a page whose score is more than 2 E above (below) the k-th largest is certainly in (out); the few in between
+// are scored again in 64 bits by the warps that have the row.  Rows with more such pages than lanes (equal scores,
+// infinities) are done in 64 bits throughout, by the whole block.
 //
-// Bound: the bounds of all pages are read once per 16 tokens (from HBM for single tokens, else from L2).
+// Single tokens are bound by reading the bounds of all pages from HBM: a block per (token, key head), a warp takes
+// eight pages at a time, 16 bytes a lane, straight into registers, the next eight under way.  Of several tokens of a sequence
+// a block scores 16 against the same pages on mma.sync, P and M as two bf16 terms each (products exact, fp32
+// sums); the bounds then come from L2 through a ring of four half stages.
 #include "cache_tma.cuh"
 
 namespace ada {
@@ -23,12 +25,14 @@ constexpr int SEL_THREADS = 256;
 constexpr int SEL_WARPS = SEL_THREADS / 32;
 constexpr int SEL_PAGES = 64;            // pages per stage: eight for every warp
 constexpr int SEL_ROWS = 16;             // tokens of a tile
+constexpr int SEL_RING = 4;              // half stages (the maxima or the minima of SEL_PAGES pages) in shared memory
 constexpr int SEL_KEYS = 16;             // scores of a row that a lane keeps in registers
-// |approximate - s(p)| <= (SEL_ERR + (G - 1) 2^-24) sum_e (P_e + |M_e|) a_e, a_e the largest |bound| of element e in any
-// page: two bf16 terms leave 2^-16 of P, its fp32 sum over G heads (G - 1) 2^-24; d_h / 16 <= 8 matrix instructions for
-// either sign add 16 products and the running sum, each of the 17 addends cut at 2^-24 of the largest.  In all 2.4e-5; the
-// sums of either sign and of the second terms, a few roundings more, are in the reserve.
-constexpr float SEL_ERR = 2.7e-5f;
+// |fp32 score - s(p)| <= (error + (G - 1) 2^-24) sum_e (P_e + |M_e|) a_e, a_e the largest |bound| of element e in any
+// page; P is an fp32 sum over G heads, (G - 1) 2^-24.
+// mma.sync: two bf16 terms leave 2^-16 of P; d_h / 16 <= 8 matrix instructions for either sign add 16 products and the
+// running sum, each of the 17 addends cut at 2^-24 of the largest: 2.4e-5; the sums of either sign and of the second
+// terms, a few roundings more, are in the reserve.  Direct: 8 fused multiply-adds and 5 additions, each rounded: 13 x 2^-24.
+constexpr float SEL_ERR_MMA = 2.7e-5f, SEL_ERR_ONE = 9e-7f;
 
 __device__ __forceinline__ unsigned long long sort_key(double x) {
     if (!(x == x)) return 0ull;                                  // NaN: behind everything
@@ -51,7 +55,8 @@ __device__ __forceinline__ void ldsm2(unsigned addr, unsigned (&r)[2]) {
 
 struct SelShared {
     double qp[128], qm[128];                       // of a row that is done in 64 bits throughout
-    unsigned col[128];                             // largest |bound| of every element (bits)
+    unsigned col[128];                             // mma.sync: largest |bound| of every element (bits)
+    unsigned reach[SEL_WARPS];                     // direct: sum_e (P_e + |M_e|) a_e, a_e over the warp's pages (bits)
     int n_hard, hard[SEL_ROWS];
     int cnt[2][SEL_WARPS], tie[SEL_WARPS];
     unsigned word[2][SEL_WARPS];
@@ -61,27 +66,33 @@ struct SelShared {
 
 // bytes of a row of d elements in shared memory: an odd number of 16-byte pieces, so that ldmatrix has no bank conflict
 __host__ __device__ __forceinline__ int sel_row(int d) { return d * 2 + 16; }
-__host__ __device__ __forceinline__ int sel_stage(int d) { return 2 * SEL_PAGES * sel_row(d); }
+__host__ __device__ __forceinline__ int sel_half(int d) { return SEL_PAGES * sel_row(d); }
 
-// grid (tiles of `rows` tokens of one sequence, key heads).  Shared memory: two stages of bounds | the tile's P and M as
-// bf16 terms | scores [rows][stride]; a row done in 64 bits throughout has its keys in the stages' place.
-__global__ void __launch_bounds__(SEL_THREADS)
-k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, int stride, int stage_room,
+// grid (tiles of `rows` tokens of one sequence, key heads).  ONE: one token per block; shared memory holds its scores.  Else:
+// the ring of half stages | the tile's P and M as bf16 terms | scores [rows][stride].  A row done in 64 bits
+// throughout has its keys at the start of it.
+template <bool ONE>
+__global__ void __launch_bounds__(SEL_THREADS, 2)
+k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, int stride, int ring_room,
                unsigned* __restrict__ status) {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ SelShared sh;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int head = blockIdx.y, G = j.h / c.h_kv;
     const int rb = sel_row(c.d);
-    unsigned char* a_tile = smem + stage_room;                  // [P hi, P lo, M hi, M lo][16][rb]
-    float* score = reinterpret_cast<float*>(a_tile + 4 * SEL_ROWS * rb);
+    unsigned char* a_tile = smem + ring_room;                   // [P hi, P lo, M hi, M lo][16][rb]
+    float* score = reinterpret_cast<float*>(ONE ? smem : a_tile + 4 * SEL_ROWS * rb);
     grid_dep_wait();
     grid_dep_launch_next();
     if (blockIdx.x == 0 && head == 0) check_ragged(r, c, status, tid, SEL_THREADS);
 
     // ---- the tile: the sequence and its first token, by every warp for itself
     int b = -1, t0 = 0;
-    {
+    if (ONE) {
+        int o;
+        b = seq_of_row(r, blockIdx.x);
+        if (b >= 0) { seq_rows(r, b, o); t0 = (int)blockIdx.x - o; }
+    } else {
         int left = blockIdx.x;
         for (int b0 = 0; b0 < r.B; b0 += 32) {
             int o;
@@ -109,117 +120,227 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
     auto limit = [&](int t) { return j.causal ? max(len - n + t0 + t + 1, 0) : len; };
     auto pages_of = [&](int t) { return (limit(t) + (1 << c.shift) - 1) >> c.shift; };
     const int nb_all = pages_of(n_tok - 1);                     // the last token sees the most
+    const int v = lane & 15, lower = lane >> 4, nvec = c.d >> 3;
     if (nb_all > j.k) {
-        // ---- loads of the bounds: a warp's lanes hold one page at a time, 16 bytes each
-        const int nvec = c.d >> 3, nst = (nb_all + SEL_PAGES - 1) / SEL_PAGES;
-        int id = -1;                                            // lane q: the table's entry for page w + 8 q of the next stage
-        auto fetch_ids = [&](int st) {
-            const int p = st * SEL_PAGES + warp + 8 * lane;
-            id = lane < 8 && p < nb_all ? page_of(c, b, p, status) : -1;
-        };
-        const int v = lane & 15, lower = lane >> 4;             // lanes 0..15 the maxima, 16..31 the minima
-        const __nv_bfloat16* bounds = (lower ? c.kmin : c.kmax) + (int64_t)head * c.d + v * 8;
-        auto load_stage = [&](int st) {
-            const unsigned at = tc::smem_u32(smem + (st & 1) * sel_stage(c.d)) + (lower * SEL_PAGES) * rb + v * 16;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const int page = __shfl_sync(0xffffffffu, id, q);
-                if (v < nvec) cp16(at + (warp + 8 * q) * rb, bounds + (int64_t)max(page, 0) * c.h_kv * c.d, page >= 0);
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
         if (tid == 0) sh.n_hard = 0;
-        if (tid < 128) sh.col[tid] = 0u;
-        __syncthreads();
-        fetch_ids(0);
-        load_stage(0);
-        if (nst > 1) fetch_ids(1);
-        // ---- P and M of the tile's tokens, two elements a thread
-        for (int i = tid; i < SEL_ROWS * (c.d >> 1); i += SEL_THREADS) {
-            const int t = i / (c.d >> 1), e = (i - t * (c.d >> 1)) * 2;
-            float p[2] = {0.f, 0.f}, m[2] = {0.f, 0.f};
-            if (t < n_tok) {
-                const __nv_bfloat16* q = j.Q + (int64_t)(row0 + t) * j.ldq + (int64_t)head * G * c.d + e;
-                for (int g = 0; g < G; ++g) {
-                    const unsigned w = *reinterpret_cast<const unsigned*>(q + (int64_t)g * c.d);
-                    const float x[2] = {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) { p[u] += fmaxf(x[u], 0.f); m[u] += fminf(x[u], 0.f); if (x[u] != x[u]) p[u] = x[u]; }
-                }
-            }
-            const __nv_bfloat162 ph = __floats2bfloat162_rn(p[0], p[1]), mh = __floats2bfloat162_rn(m[0], m[1]);
-            const __nv_bfloat162 pl = __floats2bfloat162_rn(p[0] - __low2float(ph), p[1] - __high2float(ph));
-            const __nv_bfloat162 ml = __floats2bfloat162_rn(m[0] - __low2float(mh), m[1] - __high2float(mh));
-            unsigned char* d = a_tile + t * rb + e * 2;
-            *reinterpret_cast<__nv_bfloat162*>(d) = ph;
-            *reinterpret_cast<__nv_bfloat162*>(d + SEL_ROWS * rb) = pl;
-            *reinterpret_cast<__nv_bfloat162*>(d + 2 * SEL_ROWS * rb) = mh;
-            *reinterpret_cast<__nv_bfloat162*>(d + 3 * SEL_ROWS * rb) = ml;
-        }
-        // ---- scores
-        const unsigned a_at = tc::smem_u32(a_tile) + (lane & 15) * rb + (lane >> 4) * 16;
-        __nv_bfloat162 most[4];                                  // of the elements that this lane fetches (NaN stays)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) most[u] = __float2bfloat162_rn(0.f);
-        for (int st = 0; st < nst; ++st) {
-            if (st + 1 < nst) {
-                load_stage(st + 1);
-                if (st + 2 < nst) fetch_ids(st + 2);
-                asm volatile("cp.async.wait_group 1;" ::: "memory");
-            } else {
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-            }
-            __syncthreads();
-            const unsigned char* stage = smem + (st & 1) * sel_stage(c.d);
-            if (v < nvec) {
+        if (ONE) {
+            // ---- lanes 0..15 have P and the maxima, 16..31 M and the minima, eight elements each
+            const __nv_bfloat16* bounds = (lower ? c.kmin : c.kmax) + (int64_t)head * c.d + v * 8;
+            int id = -1;                                        // lane q: the table's entry for page q of the next eight
+            auto fetch_ids = [&](int p0) {
+                const int p = p0 + warp * 8 + lane;
+                id = lane < 8 && p < nb_all ? page_of(c, b, p, status) : -1;
+            };
+            auto fetch = [&](uint4 (&x)[8]) {
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(stage + (lower * SEL_PAGES + warp + 8 * q) * rb + v * 16);
-                    const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&x);
+                    const int page = __shfl_sync(0xffffffffu, id, q);
+                    x[q] = make_uint4(0u, 0u, 0u, 0u);
+                    if (page >= 0 && v < nvec) x[q] = __ldg(reinterpret_cast<const uint4*>(bounds + (int64_t)page * c.h_kv * c.d));
+                }
+            };
+            uint4 cur[8], nxt[8];
+            fetch_ids(0);
+            fetch(cur);
+            fetch_ids(SEL_PAGES);
+            float w[8];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) most[u] = __hmax2_nan(most[u], __habs2(y[u]));
+            for (int e = 0; e < 8; ++e) w[e] = 0.f;
+            if (v < nvec) {
+                const __nv_bfloat16* q = j.Q + (int64_t)row0 * j.ldq + (int64_t)head * G * c.d + v * 8;
+#pragma unroll 4
+                for (int g = 0; g < G; ++g) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(q + (int64_t)g * c.d);
+                    const unsigned uu[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = __uint_as_float((e & 1) ? uu[e >> 1] & 0xffff0000u : uu[e >> 1] << 16);
+                        w[e] += x != x ? x : lower ? fminf(x, 0.f) : fmaxf(x, 0.f);
+                    }
                 }
             }
-            float acc[4][4];                                     // second and first terms of P, of M
+            __nv_bfloat162 most[4];                              // largest |bound| of the lane's elements (NaN stays)
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[u][i] = 0.f;
-            const unsigned b_at = tc::smem_u32(stage) + (warp * 8 + (lane & 7)) * rb + ((lane >> 3) & 1) * 16;
-            for (int ks = 0; ks < c.d >> 4; ++ks)
-#pragma unroll
-                for (int sign = 0; sign < 2; ++sign) {
-                    unsigned bf[2], hi[4], lo[4];
-                    ldsm2(b_at + sign * SEL_PAGES * rb + ks * 32, bf);
-                    tc::ldsm4(a_at + 2 * sign * SEL_ROWS * rb + ks * 32, hi);
-                    tc::ldsm4(a_at + (2 * sign + 1) * SEL_ROWS * rb + ks * 32, lo);
-                    tc::mma16816(acc[2 * sign], lo, bf[0], bf[1]);
-                    tc::mma16816(acc[2 * sign + 1], hi, bf[0], bf[1]);
+            for (int u = 0; u < 4; ++u) most[u] = __float2bfloat162_rn(0.f);
+            for (int p0 = 0; p0 < nb_all; p0 += SEL_PAGES) {
+                if (p0 + SEL_PAGES < nb_all) {
+                    fetch(nxt);
+                    fetch_ids(p0 + 2 * SEL_PAGES);
                 }
-            const int p = st * SEL_PAGES + warp * 8 + 2 * (lane & 3);
+                float a[8];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int t = (lane >> 2) + 8 * i;
-                float x[2];
+                for (int q = 0; q < 8; ++q) {
+                    const unsigned uu[4] = {cur[q].x, cur[q].y, cur[q].z, cur[q].w};
+                    a[q] = 0.f;
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    x[e] = (acc[1][2 * i + e] + acc[3][2 * i + e]) + (acc[0][2 * i + e] + acc[2][2 * i + e]);
-                if (t < n_tok) *reinterpret_cast<float2*>(score + t * stride + p) = make_float2(x[0], x[1]);
+                    for (int e = 0; e < 8; ++e)
+                        a[q] = fmaf(w[e], __uint_as_float((e & 1) ? uu[e >> 1] & 0xffff0000u : uu[e >> 1] << 16), a[q]);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) most[u] = __hmax2_nan(most[u], __habs2(*reinterpret_cast<const __nv_bfloat162*>(&uu[u])));
+                }
+                // sums of eight pages over the lanes: halves of the pages change places with halves of the lanes
+#pragma unroll
+                for (int m = 4; m > 0; m >>= 1) {
+                    const bool up = lane & (4 * m);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (q < m) {
+                            const float send = up ? a[q] : a[q + m], keep = up ? a[q + m] : a[q];
+                            a[q] = keep + __shfl_xor_sync(0xffffffffu, send, 4 * m);
+                        }
+                }
+                a[0] += __shfl_xor_sync(0xffffffffu, a[0], 2);
+                a[0] += __shfl_xor_sync(0xffffffffu, a[0], 1);
+                const int p = p0 + warp * 8 + (lane >> 2);       // (bits 4, 3, 2 of the lane: bits 2, 1, 0 of the page)
+                if ((lane & 3) == 0 && p < nb_all) score[p] = a[0];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) cur[q] = nxt[q];
+            }
+            float A = 0.f;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) A += fabsf(w[2 * u]) * __low2float(most[u]) + fabsf(w[2 * u + 1]) * __high2float(most[u]);
+#pragma unroll
+            for (int m = 16; m > 0; m >>= 1) A += __shfl_xor_sync(0xffffffffu, A, m);
+            if (lane == 0) sh.reach[warp] = __float_as_uint(A) & 0x7fffffffu;   // (a NaN's bits are larger than any number's)
+            __syncthreads();
+        } else {
+            const int nhalf = 2 * ((nb_all + SEL_PAGES - 1) / SEL_PAGES);
+            // half stage i: the maxima (i even) or minima (odd) of pages 64 (i / 2) ..; a warp's half has a page, 16 bytes a lane
+            int id = -1;                                         // lane q: the table's entry for the warp's q-th page
+            auto load_half = [&](int i) {
+                if (i < nhalf) {
+                    if ((i & 1) == 0) {
+                        const int p = (i >> 1) * SEL_PAGES + warp * 8 + lane;
+                        id = lane < 8 && p < nb_all ? page_of(c, b, p, status) : -1;
+                    }
+                    const __nv_bfloat16* bounds = ((i & 1) ? c.kmin : c.kmax) + (int64_t)head * c.d + v * 8;
+                    const unsigned at = tc::smem_u32(smem + (i & (SEL_RING - 1)) * sel_half(c.d)) + (warp * 8) * rb + v * 16;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int page = __shfl_sync(0xffffffffu, id, 2 * q + lower);
+                        if (v < nvec) cp16(at + (2 * q + lower) * rb, bounds + (int64_t)max(page, 0) * c.h_kv * c.d, page >= 0);
+                    }
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+            if (tid < 128) sh.col[tid] = 0u;
+#pragma unroll 1
+            for (int i = 0; i < SEL_RING - 1; ++i) load_half(i);
+            // ---- P and M of the tile's tokens, eight elements a thread
+            if (tid < SEL_ROWS * nvec) {
+                const int t = tid / nvec, e0 = (tid - t * nvec) * 8;
+                float p[8], m[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = m[e] = 0.f;
+                if (t < n_tok) {
+                    const __nv_bfloat16* q = j.Q + (int64_t)(row0 + t) * j.ldq + (int64_t)head * G * c.d + e0;
+#pragma unroll 4
+                    for (int g = 0; g < G; ++g) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(q + (int64_t)g * c.d);
+                        const unsigned uu[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float x = __uint_as_float((e & 1) ? uu[e >> 1] & 0xffff0000u : uu[e >> 1] << 16);
+                            p[e] += x != x ? x : fmaxf(x, 0.f);
+                            m[e] += fminf(x, 0.f);
+                        }
+                    }
+                }
+                uint4 o4[4];
+                unsigned* w = reinterpret_cast<unsigned*>(o4);
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const __nv_bfloat162 ph = __floats2bfloat162_rn(p[e], p[e + 1]), mh = __floats2bfloat162_rn(m[e], m[e + 1]);
+                    const __nv_bfloat162 pl = __floats2bfloat162_rn(p[e] - __low2float(ph), p[e + 1] - __high2float(ph));
+                    const __nv_bfloat162 ml = __floats2bfloat162_rn(m[e] - __low2float(mh), m[e + 1] - __high2float(mh));
+                    w[e >> 1] = *reinterpret_cast<const unsigned*>(&ph);
+                    w[4 + (e >> 1)] = *reinterpret_cast<const unsigned*>(&pl);
+                    w[8 + (e >> 1)] = *reinterpret_cast<const unsigned*>(&mh);
+                    w[12 + (e >> 1)] = *reinterpret_cast<const unsigned*>(&ml);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) *reinterpret_cast<uint4*>(a_tile + (u * SEL_ROWS + t) * rb + e0 * 2) = o4[u];
+            }
+            // ---- scores
+            const unsigned a_at = tc::smem_u32(a_tile) + (lane & 15) * rb + (lane >> 4) * 16;
+            __nv_bfloat162 most[4];                              // of the elements that this lane fetches (NaN stays)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) most[u] = __float2bfloat162_rn(0.f);
+            float acc[4][4];                                     // second and first terms of P, of M
+            for (int i = 0; i < nhalf; ++i) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(SEL_RING - 2) : "memory");
+                __syncthreads();                                 // half stage i is there, and nobody reads i - 1 any more
+                load_half(i + SEL_RING - 1);
+                const unsigned char* half = smem + (i & (SEL_RING - 1)) * sel_half(c.d);
+                if (v < nvec) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint4 x = *reinterpret_cast<const uint4*>(half + (warp * 8 + 2 * q + lower) * rb + v * 16);
+                        const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&x);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) most[u] = __hmax2_nan(most[u], __habs2(y[u]));
+                    }
+                }
+                const int sign = i & 1;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (sign == 0) acc[u][e] = 0.f;
+                        acc[2 + u][e] = sign == 0 ? 0.f : acc[2 + u][e];
+                    }
+                const unsigned b_at = tc::smem_u32(half) + (warp * 8 + (lane & 7)) * rb + ((lane >> 3) & 1) * 16;
+                if (sign == 0) {
+#pragma unroll 4
+                    for (int ks = 0; ks < c.d >> 4; ++ks) {
+                        unsigned bf[2], hi[4], lo[4];
+                        ldsm2(b_at + ks * 32, bf);
+                        tc::ldsm4(a_at + ks * 32, hi);
+                        tc::ldsm4(a_at + SEL_ROWS * rb + ks * 32, lo);
+                        tc::mma16816(acc[0], lo, bf[0], bf[1]);
+                        tc::mma16816(acc[1], hi, bf[0], bf[1]);
+                    }
+                } else {
+#pragma unroll 4
+                    for (int ks = 0; ks < c.d >> 4; ++ks) {
+                        unsigned bf[2], hi[4], lo[4];
+                        ldsm2(b_at + ks * 32, bf);
+                        tc::ldsm4(a_at + 2 * SEL_ROWS * rb + ks * 32, hi);
+                        tc::ldsm4(a_at + 3 * SEL_ROWS * rb + ks * 32, lo);
+                        tc::mma16816(acc[2], lo, bf[0], bf[1]);
+                        tc::mma16816(acc[3], hi, bf[0], bf[1]);
+                    }
+                    const int p = (i >> 1) * SEL_PAGES + warp * 8 + 2 * (lane & 3);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int t = (lane >> 2) + 8 * h;
+                        float x[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            x[e] = (acc[1][2 * h + e] + acc[3][2 * h + e]) + (acc[0][2 * h + e] + acc[2][2 * h + e]);
+                        if (t < n_tok) *reinterpret_cast<float2*>(score + t * stride + p) = make_float2(x[0], x[1]);
+                    }
+                }
+            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            if (v < nvec) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {                    // (a NaN's bits are larger than any number's)
+                    atomicMax(&sh.col[v * 8 + 2 * u], __float_as_uint(__low2float(most[u])) & 0x7fffffffu);
+                    atomicMax(&sh.col[v * 8 + 2 * u + 1], __float_as_uint(__high2float(most[u])) & 0x7fffffffu);
+                }
             }
             __syncthreads();
         }
-        if (v < nvec) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {                        // (a NaN's bits are larger than any number's)
-                atomicMax(&sh.col[v * 8 + 2 * u], __float_as_uint(__low2float(most[u])) & 0x7fffffffu);
-                atomicMax(&sh.col[v * 8 + 2 * u + 1], __float_as_uint(__high2float(most[u])) & 0x7fffffffu);
-            }
-        }
-        __syncthreads();
     }
 
     // ---- teams of `tw` warps, a row each: the k-th largest approximate score, and what cannot be told from it
-    const int tw = rows >= SEL_WARPS ? 1 : SEL_WARPS / rows, team = warp / tw, mate = warp - team * tw;
+    // (as many of the warps that there are for a row as keep its scores in registers: what one warp counts alone needs no
+    // meeting)
+    const int room = ONE ? SEL_WARPS : rows >= SEL_WARPS ? 1 : SEL_WARPS / rows;
+    int tw = 1;
+    while (tw < room && nb_all > SEL_KEYS * 32 * tw) tw <<= 1;
+    const int team = warp / room, mate = warp - team * room;
     const int step = 32 * tw, at0 = mate * 32 + lane;
     int turn = 0;
     auto meet = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(step) : "memory"); };
@@ -231,7 +352,7 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
         if (lane == 0) sh.cnt[turn][warp] = x;
         meet();
         x = 0;
-        for (int q = 0; q < tw; ++q) x += sh.cnt[turn][team * tw + q];
+        for (int q = 0; q < tw; ++q) x += sh.cnt[turn][team * room + q];
         return x;
     };
     auto most_of = [&](unsigned x) {
@@ -241,10 +362,10 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
         if (lane == 0) sh.word[turn][warp] = x;
         meet();
         x = 0u;
-        for (int q = 0; q < tw; ++q) x = max(x, sh.word[turn][team * tw + q]);
+        for (int q = 0; q < tw; ++q) x = max(x, sh.word[turn][team * room + q]);
         return x;
     };
-    for (int t = team; t < n_tok; t += SEL_WARPS / tw) {
+    for (int t = team; t < n_tok && mate < tw; t += SEL_WARPS / room) {
         const int nb = pages_of(t), row = row0 + t, take = min(nb, j.k);
         int32_t* idx = j.blk_idx + ((int64_t)row * c.h_kv + head) * j.k;
         if (mate == 0 && lane == 0) j.blk_cnt[(int64_t)row * c.h_kv + head] = take;
@@ -259,15 +380,27 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
         bool all_of_them = false;                                // the undecided ones are in
         if (need > 0) {
             float A = 0.f;
-            const unsigned char* ar = a_tile + t * rb;
-            for (int e = lane; e < c.d; e += 32)
-                A += (__bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(ar + e * 2)) -
-                      __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(ar + 2 * SEL_ROWS * rb + e * 2))) * __uint_as_float(sh.col[e]);
+            if (ONE) {
+                unsigned most = 0u;                              // (a page's sum is bounded by its own warp's)
+                for (int q = 0; q < SEL_WARPS; ++q) most = max(most, sh.reach[q]);
+                A = __uint_as_float(most);
+            } else {
+                if (lane * 4 < c.d) {
+                    const unsigned char* ar = a_tile + t * rb + lane * 8;
+                    const uint2 ph = *reinterpret_cast<const uint2*>(ar), mh = *reinterpret_cast<const uint2*>(ar + 2 * SEL_ROWS * rb);
+                    const uint4 a = *reinterpret_cast<const uint4*>(&sh.col[lane * 4]);
+                    A = (__uint_as_float(ph.x << 16) - __uint_as_float(mh.x << 16)) * __uint_as_float(a.x) +
+                        (__uint_as_float(ph.x & 0xffff0000u) - __uint_as_float(mh.x & 0xffff0000u)) * __uint_as_float(a.y) +
+                        (__uint_as_float(ph.y << 16) - __uint_as_float(mh.y << 16)) * __uint_as_float(a.z) +
+                        (__uint_as_float(ph.y & 0xffff0000u) - __uint_as_float(mh.y & 0xffff0000u)) * __uint_as_float(a.w);
+                }
 #pragma unroll
-            for (int m = 16; m > 0; m >>= 1) A += __shfl_xor_sync(0xffffffffu, A, m);
-            const float E = (SEL_ERR + (float)G * 6e-8f) * A * 1.004f + 1e-35f;   // (first terms are up to 2^-8 short)
+                for (int m = 16; m > 0; m >>= 1) A += __shfl_xor_sync(0xffffffffu, A, m);
+                A *= 1.004f;                                     // (first terms are up to 2^-8 short)
+            }
+            const float E = ((ONE ? SEL_ERR_ONE : SEL_ERR_MMA) + (float)G * 6e-8f) * A + 1e-35f;
             // keys, larger than 0, of the lane's first pages; 0: none
-            const bool held = last - first <= SEL_KEYS * step;
+            const bool held = last - first <= SEL_KEYS * step;   // (uniform)
             unsigned key[SEL_KEYS];
             bool odd = !(E <= 1e37f);
             unsigned lo = ~0u, hi = 0u;
@@ -314,8 +447,12 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
             const float kth = key_value(lo);
             above = __fadd_ru(kth, __fmul_ru(2.0f, E));
             below = __fadd_rd(kth, -__fmul_ru(2.0f, E));
-            int in = 0;                                          // certain ones, and 65536 for every undecided one
-            for (int p = first + at0; p < last; p += step) { const float x = s[p]; in += x > above ? 1 : x >= below ? 65536 : 0; }
+            // certain ones, and 65536 for every undecided one (keys order as the scores do)
+            int in = 0;
+            const unsigned k_above = sort_key(above), k_below = sort_key(below);
+#pragma unroll
+            for (int q = 0; q < SEL_KEYS; ++q) in += key[q] > k_above ? 1 : key[q] >= k_below ? 65536 : 0;
+            if (!held) for (int p = first + at0 + SEL_KEYS * step; p < last; p += step) { const float x = s[p]; in += x > above ? 1 : x >= below ? 65536 : 0; }
             in = sum_of(in);
             const int band = in >> 16;
             need -= in & 0xffff;
@@ -364,12 +501,12 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
                     }
 #pragma unroll
                     for (int m = 16; m > 0; m >>= 1) x += __shfl_xor_sync(0xffffffffu, x, m);
-                    if (lane == 0) sh.key[team * tw][q] = page < 0 ? 0ull : sort_key(x);
+                    if (lane == 0) sh.key[team * room][q] = page < 0 ? 0ull : sort_key(x);
                 }
                 __syncwarp();
                 if (tw > 1) meet();
                 if (mate == 0) {
-                    const unsigned long long own = lane < band ? sh.key[team * tw][lane] : 0ull;
+                    const unsigned long long own = lane < band ? sh.key[team * room][lane] : 0ull;
                     int rank = 0;
                     for (int q = 0; q < band; ++q) {
                         const unsigned long long k = __shfl_sync(0xffffffffu, own, q);
@@ -480,16 +617,22 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
 
 cudaError_t launch_cache_select(ada_ctx* ctx, const CacheView& c, const Ragged& r, const SelectJob& j, cudaStream_t s) {
     // scores of a tile: up to 64 KB, whole stages of pages
-    const int stride = (c.max_pages + SEL_PAGES - 1) / SEL_PAGES * SEL_PAGES + 4;
+    const int stride = (c.max_pages + SEL_PAGES - 1) / SEL_PAGES * SEL_PAGES + 4, keys = c.max_pages * 8;
     int rows = SEL_ROWS;
     while (rows > 1 && (rows * stride * 4 > 65536 || rows / 2 * (int64_t)r.B >= r.N)) rows >>= 1;
-    const int keys = c.max_pages * 8, stages = 2 * sel_stage(c.d);
-    const int room = ((keys > stages ? keys : stages) + 15) / 16 * 16;
+    const int most = 226 * 1024 - (int)sizeof(SelShared);
+    if (rows == 1) {
+        const cudaError_t e = allow_smem(ctx, 14, k_cache_select<true>, most);
+        if (e != cudaSuccess) return e;
+        return launch_k(ctx, k_cache_select<true>, dim3(r.N, c.h_kv), dim3(SEL_THREADS), (keys + 15) / 16 * 16, s, c, r, j, 1, stride,
+                        0, ctx->status);
+    }
+    const int ring = SEL_RING * sel_half(c.d), room = ((keys > ring ? keys : ring) + 15) / 16 * 16;
     const int smem = room + 4 * SEL_ROWS * sel_row(c.d) + rows * stride * 4;
-    cudaError_t e = allow_smem(ctx, 14, k_cache_select, 226 * 1024 - (int)sizeof(SelShared));
+    const cudaError_t e = allow_smem(ctx, 15, k_cache_select<false>, most);
     if (e != cudaSuccess) return e;
-    return launch_k(ctx, k_cache_select, dim3(r.N / rows + (rows > 1 ? (r.B < r.N ? r.B : r.N) : 0), c.h_kv), dim3(SEL_THREADS), smem, s, c, r, j, rows,
-                    stride, room, ctx->status);
+    return launch_k(ctx, k_cache_select<false>, dim3(r.N / rows + (r.B < r.N ? r.B : r.N), c.h_kv), dim3(SEL_THREADS), smem, s, c, r, j,
+                    rows, stride, room, ctx->status);
 }
 
 }  // namespace ada
