@@ -26,7 +26,8 @@ constexpr int SEL_WARPS = SEL_THREADS / 32;
 constexpr int SEL_PAGES = 64;            // pages per stage: eight for every warp
 constexpr int SEL_ROWS = 16;             // tokens of a tile
 constexpr int SEL_RING = 4;              // half stages (the maxima or the minima of SEL_PAGES pages) in shared memory
-constexpr int SEL_KEYS = 16;             // scores of a row that a lane keeps in registers
+constexpr int SEL_SPAN = 512;            // scores of a row that one warp counts alone
+constexpr float SEL_NONE = -3.402823466e38f;   // of pages that do not compete
 // |fp32 score - s(p)| <= (error + (G - 1) 2^-24) sum_e (P_e + |M_e|) a_e, a_e the largest |bound| of element e in any
 // page; P is an fp32 sum over G heads, (G - 1) 2^-24.
 // mma.sync: two bf16 terms leave 2^-16 of P; d_h / 16 <= 8 matrix instructions for either sign add 16 products and the
@@ -334,17 +335,16 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
         }
     }
 
-    // ---- teams of `tw` warps, a row each: the k-th largest approximate score, and what cannot be told from it
-    // (as many of the warps that there are for a row as keep its scores in registers: what one warp counts alone needs no
-    // meeting)
+    // ---- teams of `tw` warps, a row each: the k-th largest fp32 score, and what cannot be told from it
+    // (One warp alone needs no meeting.  Four scores a lane and load; the code is kept small, every block runs it once.)
     const int room = ONE ? SEL_WARPS : rows >= SEL_WARPS ? 1 : SEL_WARPS / rows;
     int tw = 1;
-    while (tw < room && nb_all > SEL_KEYS * 32 * tw) tw <<= 1;
+    while (tw < room && nb_all > SEL_SPAN * tw) tw <<= 1;
     const int team = warp / room, mate = warp - team * room;
     const int step = 32 * tw, at0 = mate * 32 + lane;
     int turn = 0;
     auto meet = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(step) : "memory"); };
-    // sum (least, greatest) over the team; the slots alternate, so that one meeting per call is enough
+    // sum (greatest) over the team; the slots alternate, so that one meeting per call is enough
     auto sum_of = [&](int x) {
         x = __reduce_add_sync(0xffffffffu, x);
         if (tw == 1) return x;
@@ -374,162 +374,156 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
             continue;
         }
         float* s = score + t * stride;
+        const float4* s4 = reinterpret_cast<const float4*>(s);
         const int first = j.n_first, last = nb - j.n_last;       // pages [first, last) compete for `need` places
+        const int n4 = (nb + 3) >> 2;                            // float4s of the row
+        // the others are out of it, and listed without further ado
+        for (int p = at0; p < first; p += step) { s[p] = SEL_NONE; idx[p] = p; }
+        for (int p = last + at0; p < n4 * 4; p += step) {
+            s[p] = SEL_NONE;
+            if (p < nb) idx[j.k - nb + p] = p;
+        }
+        if (tw > 1) meet(); else __syncwarp();
         int need = j.k - j.n_first - j.n_last;
-        float above = INFINITY, below = INFINITY;                // undecided if below <= s <= above
-        bool all_of_them = false;                                // the undecided ones are in
-        if (need > 0) {
-            float A = 0.f;
-            if (ONE) {
-                unsigned most = 0u;                              // (a page's sum is bounded by its own warp's)
-                for (int q = 0; q < SEL_WARPS; ++q) most = max(most, sh.reach[q]);
-                A = __uint_as_float(most);
-            } else {
-                if (lane * 4 < c.d) {
-                    const unsigned char* ar = a_tile + t * rb + lane * 8;
-                    const uint2 ph = *reinterpret_cast<const uint2*>(ar), mh = *reinterpret_cast<const uint2*>(ar + 2 * SEL_ROWS * rb);
-                    const uint4 a = *reinterpret_cast<const uint4*>(&sh.col[lane * 4]);
-                    A = (__uint_as_float(ph.x << 16) - __uint_as_float(mh.x << 16)) * __uint_as_float(a.x) +
-                        (__uint_as_float(ph.x & 0xffff0000u) - __uint_as_float(mh.x & 0xffff0000u)) * __uint_as_float(a.y) +
-                        (__uint_as_float(ph.y << 16) - __uint_as_float(mh.y << 16)) * __uint_as_float(a.z) +
-                        (__uint_as_float(ph.y & 0xffff0000u) - __uint_as_float(mh.y & 0xffff0000u)) * __uint_as_float(a.w);
+        if (need == 0) continue;
+        float A = 0.f;
+        if (ONE) {                                               // (a page's sum is bounded by its own warp's)
+            A = __uint_as_float(__reduce_max_sync(0xffffffffu, sh.reach[lane & (SEL_WARPS - 1)]));
+        } else {
+            if (lane * 4 < c.d) {
+                const unsigned char* ar = a_tile + t * rb + lane * 8;
+                const uint2 ph = *reinterpret_cast<const uint2*>(ar), mh = *reinterpret_cast<const uint2*>(ar + 2 * SEL_ROWS * rb);
+                const uint4 a = *reinterpret_cast<const uint4*>(&sh.col[lane * 4]);
+                A = (__uint_as_float(ph.x << 16) - __uint_as_float(mh.x << 16)) * __uint_as_float(a.x) +
+                    (__uint_as_float(ph.x & 0xffff0000u) - __uint_as_float(mh.x & 0xffff0000u)) * __uint_as_float(a.y) +
+                    (__uint_as_float(ph.y << 16) - __uint_as_float(mh.y << 16)) * __uint_as_float(a.z) +
+                    (__uint_as_float(ph.y & 0xffff0000u) - __uint_as_float(mh.y & 0xffff0000u)) * __uint_as_float(a.w);
+            }
+#pragma unroll
+            for (int m = 16; m > 0; m >>= 1) A += __shfl_xor_sync(0xffffffffu, A, m);
+            A *= 1.004f;                                         // (first terms are up to 2^-8 short)
+        }
+        // no score is larger than A and its error: beyond this, or for a NaN, fp32 says nothing
+        if (!(A <= 1e36f)) {
+            if (mate == 0 && lane == 0) sh.hard[atomicAdd(&sh.n_hard, 1)] = t;
+            continue;
+        }
+        const float E = ((ONE ? SEL_ERR_ONE : SEL_ERR_MMA) + (float)G * 6e-8f) * A + 1e-35f;
+        float mn = INFINITY, mx = SEL_NONE;
+        for (int i = at0; i < n4; i += step) {
+            const float4 x = s4[i];
+            mx = fmaxf(mx, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)));
+            mn = fminf(mn, fminf(fminf(x.x == SEL_NONE ? mn : x.x, x.y == SEL_NONE ? mn : x.y), fminf(x.z == SEL_NONE ? mn : x.z, x.w == SEL_NONE ? mn : x.w)));
+        }
+        // at least `need` scores are >= lo, fewer than that > hi (as keys: integers that order as the scores do)
+        unsigned hi = most_of(sort_key(mx)), lo = ~most_of(~sort_key(mn));
+        while (lo < hi) {
+            const unsigned mid = lo + ((hi - lo + 1u) >> 1);
+            const float at = key_value(mid);
+            int ge = 0;
+#pragma unroll 2
+            for (int i = at0; i < n4; i += step) {
+                const float4 x = s4[i];
+                ge += (x.x >= at) + (x.y >= at) + (x.z >= at) + (x.w >= at);
+            }
+            ge = sum_of(ge);
+            if (ge >= need) lo = mid; else hi = mid - 1u;
+            if (ge == need) {                                    // the smallest of them is the one that is sought
+                mn = INFINITY;
+                for (int i = at0; i < n4; i += step) {
+                    const float4 x = s4[i];
+                    mn = fminf(mn, fminf(fminf(x.x >= at ? x.x : mn, x.y >= at ? x.y : mn), fminf(x.z >= at ? x.z : mn, x.w >= at ? x.w : mn)));
+                }
+                lo = ~most_of(~sort_key(mn));
+                break;
+            }
+        }
+        // undecided if below <= s <= above
+        const float kth = key_value(lo), above = __fadd_ru(kth, __fmul_ru(2.0f, E)), below = __fadd_rd(kth, -__fmul_ru(2.0f, E));
+        int in = 0;                                              // certain ones, and 65536 for every undecided one
+        for (int i = at0; i < n4; i += step) {
+            const float4 x = s4[i];
+            in += (x.x > above ? 1 : x.x >= below ? 65536 : 0) + (x.y > above ? 1 : x.y >= below ? 65536 : 0) +
+                  (x.z > above ? 1 : x.z >= below ? 65536 : 0) + (x.w > above ? 1 : x.w >= below ? 65536 : 0);
+        }
+        in = sum_of(in);
+        const int band = in >> 16;
+        need -= in & 0xffff;
+        // places of the pages of 32 float4s for which `is` holds, ascending: what a warp writes them with
+        auto list = [&](auto is, auto put) {
+            int n_put = 0;
+            for (int i0 = 0; i0 < n4; i0 += 32) {
+                const float4 x = i0 + lane < n4 ? s4[i0 + lane] : make_float4(SEL_NONE, SEL_NONE, SEL_NONE, SEL_NONE);
+                const bool y[4] = {is(x.x), is(x.y), is(x.z), is(x.w)};
+                int before = n_put;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned m = __ballot_sync(0xffffffffu, y[e]);
+                    before += __popc(m & ((1u << lane) - 1u));
+                    n_put += __popc(m);
                 }
 #pragma unroll
-                for (int m = 16; m > 0; m >>= 1) A += __shfl_xor_sync(0xffffffffu, A, m);
-                A *= 1.004f;                                     // (first terms are up to 2^-8 short)
+                for (int e = 0; e < 4; ++e)
+                    if (y[e]) put(before++, 4 * (i0 + lane) + e);
             }
-            const float E = ((ONE ? SEL_ERR_ONE : SEL_ERR_MMA) + (float)G * 6e-8f) * A + 1e-35f;
-            // keys, larger than 0, of the lane's first pages; 0: none
-            const bool held = last - first <= SEL_KEYS * step;   // (uniform)
-            unsigned key[SEL_KEYS];
-            bool odd = !(E <= 1e37f);
-            unsigned lo = ~0u, hi = 0u;
-#pragma unroll
-            for (int q = 0; q < SEL_KEYS; ++q) {
-                const int p = first + at0 + q * step;
-                key[q] = 0u;
-                if (p < last) {
-                    const float x = s[p];
-                    odd = odd || !(fabsf(x) <= 1e37f);
-                    key[q] = sort_key(x);
-                    lo = min(lo, key[q]); hi = max(hi, key[q]);
-                }
-            }
-            for (int p = first + at0 + SEL_KEYS * step; p < last; p += step) {
-                const float x = s[p];
-                odd = odd || !(fabsf(x) <= 1e37f);
-                lo = min(lo, sort_key(x)); hi = max(hi, sort_key(x));
-            }
-            hi = most_of(odd ? ~0u : hi);
-            if (hi == ~0u) {                                     // (no finite score has that key)
+        };
+        float cut = below;                                       // in the end: in if s >= cut
+        if (band != need) {
+            if (band > 32) {
                 if (mate == 0 && lane == 0) sh.hard[atomicAdd(&sh.n_hard, 1)] = t;
                 continue;
             }
-            lo = ~most_of(~lo);
-            // at least `need` keys are >= lo, fewer than that > hi
-            while (lo < hi) {
-                const unsigned mid = lo + ((hi - lo + 1u) >> 1);
-                int ge = 0;
+            // every warp of the team lists them; each scores its share of them in 64 bits
+            list([&](float x) { return x >= below && x <= above; }, [&](int at, int p) { sh.list[warp][at] = p; });
+            __syncwarp();
+            const int mine = lane < band ? sh.list[warp][lane] : INT_MAX;
+            const int page_l = lane < band ? page_of(c, b, mine, status) : -1;
+            double P[4], M[4];                                   // of elements 4 lane .. 4 lane + 3
+            const bool on = lane * 4 < c.d;
 #pragma unroll
-                for (int q = 0; q < SEL_KEYS; ++q) ge += key[q] >= mid;
-                if (!held) for (int p = first + at0 + SEL_KEYS * step; p < last; p += step) ge += sort_key(s[p]) >= mid;
-                ge = sum_of(ge);
-                if (ge >= need) lo = mid; else hi = mid - 1u;
-                if (ge == need) {                                // the smallest of them is the one that is sought
-                    unsigned least = ~0u;
+            for (int e = 0; e < 4; ++e) P[e] = M[e] = 0.0;
+            const __nv_bfloat16* qrow = j.Q + (int64_t)row * j.ldq + (int64_t)head * G * c.d + lane * 4;
+            for (int g = 0; g < G && on; ++g) {
+                const uint2 w = *reinterpret_cast<const uint2*>(qrow + (int64_t)g * c.d);
 #pragma unroll
-                    for (int q = 0; q < SEL_KEYS; ++q) if (key[q] >= mid) least = min(least, key[q]);
-                    if (!held) for (int p = first + at0 + SEL_KEYS * step; p < last; p += step) { const unsigned k = sort_key(s[p]); if (k >= mid) least = min(least, k); }
-                    lo = ~most_of(~least);
-                    break;
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned u = e < 2 ? w.x : w.y;
+                    const double x = (double)__uint_as_float((e & 1) ? u & 0xffff0000u : u << 16);
+                    P[e] += x > 0.0 ? x : 0.0;
+                    M[e] += x > 0.0 ? 0.0 : x;
                 }
             }
-            const float kth = key_value(lo);
-            above = __fadd_ru(kth, __fmul_ru(2.0f, E));
-            below = __fadd_rd(kth, -__fmul_ru(2.0f, E));
-            // certain ones, and 65536 for every undecided one (keys order as the scores do)
-            int in = 0;
-            const unsigned k_above = sort_key(above), k_below = sort_key(below);
-#pragma unroll
-            for (int q = 0; q < SEL_KEYS; ++q) in += key[q] > k_above ? 1 : key[q] >= k_below ? 65536 : 0;
-            if (!held) for (int p = first + at0 + SEL_KEYS * step; p < last; p += step) { const float x = s[p]; in += x > above ? 1 : x >= below ? 65536 : 0; }
-            in = sum_of(in);
-            const int band = in >> 16;
-            need -= in & 0xffff;
-            if (band == need) {
-                all_of_them = true;
-            } else if (band <= 32) {
-                // every warp of the team lists them; each scores its share of them in 64 bits
-                int at = 0;
-                for (int p0 = first; p0 < last; p0 += 32) {
-                    const int p = p0 + lane;
-                    const bool is = p < last && s[p] >= below && s[p] <= above;
-                    const unsigned m = __ballot_sync(0xffffffffu, is);
-                    if (is) sh.list[warp][at + __popc(m & ((1u << lane) - 1u))] = p;
-                    at += __popc(m);
-                }
-                __syncwarp();
-                const int mine = lane < band ? sh.list[warp][lane] : INT_MAX;
-                const int page_l = lane < band ? page_of(c, b, mine, status) : -1;
-                double P[4], M[4];                               // of elements 4 lane .. 4 lane + 3
-                const bool on = lane * 4 < c.d;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) P[e] = M[e] = 0.0;
-                const __nv_bfloat16* qrow = j.Q + (int64_t)row * j.ldq + (int64_t)head * G * c.d + lane * 4;
-                for (int g = 0; g < G && on; ++g) {
-                    const uint2 w = *reinterpret_cast<const uint2*>(qrow + (int64_t)g * c.d);
+            for (int q = mate; q < band; q += tw) {
+                const int page = __shfl_sync(0xffffffffu, page_l, q);
+                double x = 0.0;
+                if (page >= 0 && on) {
+                    const int64_t base = ((int64_t)page * c.h_kv + head) * c.d + lane * 4;
+                    const uint2 u = *reinterpret_cast<const uint2*>(c.kmax + base), z = *reinterpret_cast<const uint2*>(c.kmin + base);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const unsigned u = e < 2 ? w.x : w.y;
-                        const double x = (double)__uint_as_float((e & 1) ? u & 0xffff0000u : u << 16);
-                        P[e] += x > 0.0 ? x : 0.0;
-                        M[e] += x > 0.0 ? 0.0 : x;
+                        const unsigned a = e < 2 ? u.x : u.y, i = e < 2 ? z.x : z.y;
+                        x = fma(P[e], (double)__uint_as_float((e & 1) ? a & 0xffff0000u : a << 16),
+                                fma(M[e], (double)__uint_as_float((e & 1) ? i & 0xffff0000u : i << 16), x));
                     }
                 }
-                for (int q = mate; q < band; q += tw) {
-                    const int page = __shfl_sync(0xffffffffu, page_l, q);
-                    double x = 0.0;
-                    if (page >= 0 && on) {
-                        const int64_t base = ((int64_t)page * c.h_kv + head) * c.d + lane * 4;
-                        const uint2 u = *reinterpret_cast<const uint2*>(c.kmax + base), z = *reinterpret_cast<const uint2*>(c.kmin + base);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const unsigned a = e < 2 ? u.x : u.y, i = e < 2 ? z.x : z.y;
-                            x = fma(P[e], (double)__uint_as_float((e & 1) ? a & 0xffff0000u : a << 16),
-                                    fma(M[e], (double)__uint_as_float((e & 1) ? i & 0xffff0000u : i << 16), x));
-                        }
-                    }
-#pragma unroll
-                    for (int m = 16; m > 0; m >>= 1) x += __shfl_xor_sync(0xffffffffu, x, m);
-                    if (lane == 0) sh.key[team * room][q] = page < 0 ? 0ull : sort_key(x);
-                }
-                __syncwarp();
-                if (tw > 1) meet();
-                if (mate == 0) {
-                    const unsigned long long own = lane < band ? sh.key[team * room][lane] : 0ull;
-                    int rank = 0;
-                    for (int q = 0; q < band; ++q) {
-                        const unsigned long long k = __shfl_sync(0xffffffffu, own, q);
-                        rank += k > own || (k == own && q < lane);   // (the list ascends)
-                    }
-                    if (lane < band) s[mine] = rank < need ? INFINITY : -INFINITY;
-                }
-                __syncwarp();
-            } else {
-                if (mate == 0 && lane == 0) sh.hard[atomicAdd(&sh.n_hard, 1)] = t;
-                continue;
+                for (int m = 16; m > 0; m >>= 1) x += __shfl_xor_sync(0xffffffffu, x, m);
+                if (lane == 0) sh.key[team * room][q] = page < 0 ? 0ull : sort_key(x);
             }
-        }
-        if (mate == 0) {                                         // (the first warp has what was decided in 64 bits)
-            int at = 0;
-            for (int p0 = 0; p0 < nb; p0 += 32) {
-                const int p = p0 + lane;
-                const bool in = p < nb && (p < first || p >= last || (all_of_them ? s[p] >= below : s[p] > above));
-                const unsigned m = __ballot_sync(0xffffffffu, in);
-                if (in) idx[at + __popc(m & ((1u << lane) - 1u))] = p;
-                at += __popc(m);
+            if (tw > 1) meet(); else __syncwarp();
+            const unsigned long long own = lane < band ? sh.key[team * room][lane] : 0ull;
+            int rank = 0;
+            for (int q = 0; q < band; ++q) {
+                const unsigned long long k = __shfl_sync(0xffffffffu, own, q);
+                rank += k > own || (k == own && q < lane);       // (the list ascends)
             }
+            if (mate == 0 && lane < band) s[mine] = rank < need ? -SEL_NONE : SEL_NONE;
+            __syncwarp();
+            cut = __uint_as_float(__float_as_uint(above) + (above >= 0.f ? 1u : -1u));   // (the next number above it)
+            if (above == 0.f) cut = 1.4e-45f;
         }
+        if (mate == 0)                                           // (the first warp has what was decided in 64 bits)
+            list([&](float x) { return x >= cut; }, [&](int at, int p) { idx[first + at] = p; });
     }
     if (nb_all <= j.k) return;
     __syncthreads();
@@ -624,7 +618,8 @@ cudaError_t launch_cache_select(ada_ctx* ctx, const CacheView& c, const Ragged& 
     if (rows == 1) {
         const cudaError_t e = allow_smem(ctx, 14, k_cache_select<true>, most);
         if (e != cudaSuccess) return e;
-        return launch_k(ctx, k_cache_select<true>, dim3(r.N, c.h_kv), dim3(SEL_THREADS), (keys + 15) / 16 * 16, s, c, r, j, 1, stride,
+        return launch_k(ctx, k_cache_select<true>, dim3(r.N, c.h_kv), dim3(SEL_THREADS), ((keys > stride * 4 ? keys : stride * 4) + 15) / 16 * 16, s, c, r, j, 1,
+                        stride,
                         0, ctx->status);
     }
     const int ring = SEL_RING * sel_half(c.d), room = ((keys > ring ? keys : ring) + 15) / 16 * 16;
