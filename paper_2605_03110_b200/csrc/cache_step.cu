@@ -25,23 +25,26 @@ using namespace tc;
 
 namespace {
 
-constexpr int ST_WARPS = 8;
-constexpr int ST_THREADS = 32 * ST_WARPS;
+constexpr int ST_WARPS = 8;                // warps of a team; teams of one warp: st_warps of them in a CTA
+constexpr int ST_MOST = 12;
 constexpr int GK = 32;                     // keys per granule
 constexpr int UNIT = GK * ST_WARPS;        // keys per unit of dense work
 constexpr int NOWHERE = 0x7fff0000;        // position of keys that are not there: behind every limit
 constexpr int SLOT_FLOATS = 16 * 128 + 32; // one partial result: 16 rows x 128, maxima, sums
 constexpr float ST_LAG = 8.0f;
 
+// Warps of a CTA: lone warps with up to 8 rows need few enough registers for twelve, with two slots each instead of three
+// (1000 tokens x 8 key heads, lists of 16 pages of 64: 292 -> 244 us, 17 TB/s out of L2).
+template <int NT, int TEAM> __host__ __device__ constexpr int st_warps() { return TEAM == 1 && NT == 1 ? 12 : 8; }
 // slots of a warp's ring: K or V of a granule, NDB blocks of 64 elements x 32 keys
-template <int NDB> __host__ __device__ constexpr int st_slots() { return 6 / NDB; }
+template <int NDB, int NT, int TEAM> __host__ __device__ constexpr int st_slots() { return (st_warps<NT, TEAM>() == 12 ? 4 : 6) / NDB; }
 template <int NDB> __host__ __device__ constexpr int st_slot_bytes() { return NDB * GK * 128; }
-template <int NDB> __host__ __device__ constexpr int st_ring_bytes() { return ST_WARPS * st_slots<NDB>() * st_slot_bytes<NDB>(); }
+template <int NDB> __host__ __device__ constexpr int st_ring_bytes() { return 48 / NDB * st_slot_bytes<NDB>(); }   // 12 x 4 = 8 x 6 = 48
 template <int NDB> __host__ __device__ constexpr int st_merge_bytes() { return ST_WARPS * 8 * NDB * 64 * 4; }
 
 struct StepShared {
-    unsigned long long full[ST_WARPS][6];
-    int2 base[ST_WARPS][6];                // positions of the two halves of a granule
+    unsigned long long full[ST_MOST][6];
+    int2 base[ST_MOST][6];                // positions of the two halves of a granule
     float m[ST_WARPS][16], l[ST_WARPS][16];
     int abort_flag[2];
     int last;
@@ -152,10 +155,10 @@ __device__ __forceinline__ float* partial(float* ws, const Seg& s, int piece) {
 
 // NT: rows / 8
 template <int NDB, int NT, bool LIST, int TEAM>
-__global__ void __launch_bounds__(ST_THREADS, 1)
+__global__ void __launch_bounds__(32 * st_warps<NT, TEAM>(), 1)
 k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Ragged r, const AttendJob j, int tiles,
              int pieces, float* __restrict__ ws, unsigned* __restrict__ counters, unsigned* __restrict__ status) {
-    constexpr int SLOTS = st_slots<NDB>();
+    constexpr int SLOTS = st_slots<NDB, NT, TEAM>(), WARPS = st_warps<NT, TEAM>(), THREADS = 32 * WARPS;
     constexpr int KS = NDB * 4;                       // 16-element steps of a head row
     constexpr int BLOCK = GK * 128;                   // one 64-element block of 32 keys: 4 KiB
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -183,7 +186,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
     __syncthreads();
     grid_dep_wait();
     grid_dep_launch_next();
-    if (blockIdx.x == 0) check_ragged(r, c, status, tid, ST_THREADS);
+    if (blockIdx.x == 0) check_ragged(r, c, status, tid, THREADS);
 
     // ---------------------------------------------------------------- this team's run of work
     const int w = TEAM == 1 ? 0 : warp;
@@ -192,8 +195,8 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
     work.head = work.n = work.off = work.len = work.ku = work.nu = work.row = work.rt = work.piece = 0;
     if (LIST) {
         const int64_t items = (int64_t)r.N * c.h_kv * tiles * pieces;
-        const int64_t teams = (int64_t)gridDim.x * (ST_WARPS / TEAM);
-        const int64_t team = (int64_t)blockIdx.x * (ST_WARPS / TEAM) + (TEAM == 1 ? warp : 0);
+        const int64_t teams = (int64_t)gridDim.x * (WARPS / TEAM);
+        const int64_t team = (int64_t)blockIdx.x * (WARPS / TEAM) + (TEAM == 1 ? warp : 0);
         work.per = (items + teams - 1) / teams;
         work.at = min(team * work.per, items);
         work.end = min(work.at + work.per, items);
@@ -538,7 +541,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                     mrg[(warp * 8 + c0 + (e & 1)) * W + d * 16 + (e >> 1) * 8 + r0] = o[d][nt][e];
             __syncthreads();
             const int rows = min(s.rows - nt * 8, 8);
-            for (int rr = tid / W; rr < rows; rr += ST_THREADS / W) {
+            for (int rr = tid / W; rr < rows; rr += THREADS / W) {
                 const int row = nt * 8 + rr;
                 float M = -INFINITY, L = 0.f, x = 0.f;
 #pragma unroll
@@ -569,7 +572,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
             __syncthreads();
             if (sh.last) {                             // the others' results are there: join them in the order of the keys
                 __threadfence();
-                for (int row = tid / W; row < s.rows; row += ST_THREADS / W) {
+                for (int row = tid / W; row < s.rows; row += THREADS / W) {
                     float M = -INFINITY, L = 0.f, x = 0.f;
                     for (int p = 0; p < s.pieces; ++p) M = fmaxf(M, __ldcg(partial<LIST>(ws, s, p) + 2048 + row));
                     const float ref = M > -INFINITY ? M : 0.f;
@@ -607,7 +610,7 @@ cudaError_t run_step(ada_ctx* ctx, const StepMaps& maps, const CacheView& c, con
     auto kernel = k_cache_step<NDB, NT, LIST, TEAM>;
     cudaError_t e = allow_smem(ctx, (NDB - 1) + 2 * (NT - 1) + 4 * (!LIST ? 0 : TEAM == 1 ? 1 : 2), kernel, st_smem<NDB>());   // bits 0 .. 11
     if (e != cudaSuccess) return e;
-    return launch_k(ctx, kernel, dim3(p.grid), dim3(ST_THREADS), st_smem<NDB>(), s, maps, c, r, j, p.tiles, p.pieces,
+    return launch_k(ctx, kernel, dim3(p.grid), dim3(32 * st_warps<NT, TEAM>()), st_smem<NDB>(), s, maps, c, r, j, p.tiles, p.pieces,
                     ctx->cache_part, ctx->cache_ctr, ctx->status);
 }
 template <bool LIST, int TEAM>
