@@ -100,10 +100,9 @@ struct ChunkWork {
         it.ku = ku;
         it.take = (int)min((long long)(nu - ku), end - at);
         const long long first = at - ku;
-        it.c0 = (int)(first / per);
-        it.c1 = (int)((first + nu - 1) / per);
+        shares_of(first, nu, per, blockIdx.x, it.c0, it.c1);
         it.pieces = it.c1 - it.c0 + 1;
-        it.piece = (int)(at / per) - it.c0;
+        it.piece = (int)blockIdx.x - it.c0;
         at += it.take; ku += it.take;
         return true;
     }
@@ -584,20 +583,33 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     for (int p = 0; p < it.pieces; ++p)
                         L = fmaf(__ldcg(part(p) + 128 * 256 + 256 + at), ex2_approx(__ldcg(part(p) + 128 * 256 + at) - Mr), L);
                     const float f = L > 0.f ? 1.0f / L : 0.f;
+                    // 32 columns of a piece in flight; the own piece's are still in TMEM, the same numbers
 #pragma unroll 1
-                    for (int q = 0; q < NDB * 2; ++q) {                      // 32 columns of a piece in flight
+                    for (int q = 0; q < NDB * 2; ++q) {
                         if (q * 32 >= c.d) break;
                         float y[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) y[e] = 0.f;
 #pragma unroll 1
                         for (int p = 0; p < it.pieces; ++p) {
-                            const float4* o = reinterpret_cast<const float4*>(part(p)) + q * 8 * 256 + at;
-                            const float mp = __ldcg(part(p) + 128 * 256 + at);
                             float4 z[8];
+                            if (p == it.piece) {
+                                unsigned x[32];
+                                if (nt > 0) { tmem_ld32_issue(t_o + q * 32, x); tmem_ld_wait(x); }
+                                else {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) z[e] = __ldcg(o + e * 256);
-                            const float fp = ex2_approx(mp - Mr);
+                                    for (int e = 0; e < 32; ++e) x[e] = 0u;
+                                }
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    z[e] = make_float4(__uint_as_float(x[4 * e]), __uint_as_float(x[4 * e + 1]),
+                                                       __uint_as_float(x[4 * e + 2]), __uint_as_float(x[4 * e + 3]));
+                            } else {
+                                const float4* o = reinterpret_cast<const float4*>(part(p)) + q * 8 * 256 + at;
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) z[e] = __ldcg(o + e * 256);
+                            }
+                            const float fp = ex2_approx((p == it.piece ? m : __ldcg(part(p) + 128 * 256 + at)) - Mr);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
                                 y[4 * e] = fmaf(z[e].x, fp, y[4 * e]); y[4 * e + 1] = fmaf(z[e].y, fp, y[4 * e + 1]);

@@ -76,6 +76,17 @@ static __device__ __forceinline__ int page_of(const CacheView& c, int b, int p, 
     atomicOr(status, ST_BAD_INDEX);
     return -1;
 }
+// Units [first, first + n) of a job dealt out in runs of `per`, seen from CTA `c`, whose run has some of them: the first CTA
+// with any of them and the last one.  (32-bit divisions: n is a few thousand, `per` may be anything.)
+static __device__ __forceinline__ void shares_of(int64_t first, int n, int64_t per, int c, int& c0, int& c1) {
+    const unsigned p32 = per > 0x7fffffff ? 0x7fffffffu : (unsigned)per;
+    const int64_t mine = per * c;
+    const int before = (int)(first < mine ? mine - first : 0);              // of them in front of the run, behind it
+    const int64_t end = first + n - (mine + per);
+    const int after = (int)(end > 0 ? end : 0);
+    c0 = c - (int)(((unsigned)before + p32 - 1u) / p32);
+    c1 = c + (int)(((unsigned)after + p32 - 1u) / p32);
+}
 static __device__ __forceinline__ int64_t slot_at(const CacheView& c, int page, int head, int slot) {
     return (int64_t)page * c.page_stride + ((int64_t)(head << c.shift) + slot) * c.d;
 }

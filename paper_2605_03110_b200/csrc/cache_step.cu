@@ -134,9 +134,10 @@ struct Work {                              // where a team is in its run of work
         if (take == nu) {
             s.pieces = 1; s.piece = s.slot0 = s.ctr = 0;
         } else {
-            const int c0 = (int)(first / per), c1 = (int)((first + nu - 1) / per);
+            int c0, c1;
+            shares_of(first, nu, per, blockIdx.x, c0, c1);
             s.pieces = c1 - c0 + 1;
-            s.piece = (int)(at / per) - c0;
+            s.piece = (int)blockIdx.x - c0;
             s.slot0 = c0;
             s.ctr = c1;
         }
