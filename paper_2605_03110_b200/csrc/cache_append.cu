@@ -12,7 +12,9 @@
 // rotation pairs with each other, so that it needs nobody else's elements, and keeps the four sines and cosines of
 // its pairs, and the norm's weights, in registers for all heads of the token.
 //
-// The bounds of a page need all of its keys.  Calls of several tokens each form them in a second kernel, from the pages.  Where
+// The bounds of a page need all of its keys.  Calls of several tokens each form them in a second kernel, from the pages (12
+// of 70 us for 6660 tokens of 3 x 32 heads of 128; a kernel that took the keys page by page and kept the bounds on the way was
+// slower, 76: a page's tokens are too few warps).  Where
 // there are no more tokens than sequences (a decoding step) the second launch would take as long as the first: there a
 // warp of its own takes each key head of a token and reads the page's older keys beside the new one; should several new
 // tokens lie in a page, the last one's warp forms the others' keys once more.
@@ -22,7 +24,7 @@ namespace ada {
 
 namespace {
 
-constexpr int APP_THREADS = 256;
+constexpr int APP_THREADS = 128;
 constexpr int APP_WARPS = APP_THREADS / 32;
 constexpr int APP_ROWS = 4;              // rows of a group in flight
 
@@ -134,7 +136,7 @@ __device__ __forceinline__ void widen(uint2& lo, uint2& hi, const uint2& a, cons
 // A warp: one token, or one of `shares` parts of its heads.  LG lanes have a head's row.  STEP: after the queries' shares every
 // key head of the token has a warp of its own, which also forms the page's bounds.
 template <int LG, bool PAIRS, bool STEP>
-__global__ void __launch_bounds__(APP_THREADS)
+__global__ void __launch_bounds__(APP_THREADS, 6)
 k_cache_append(const CacheView c, const Ragged r, const AppendJob j, int shares, unsigned* __restrict__ status) {
     grid_dep_wait();
     grid_dep_launch_next();
