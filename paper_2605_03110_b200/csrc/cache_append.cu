@@ -287,8 +287,6 @@ constexpr int BND_THREADS = 128;
 __global__ void __launch_bounds__(BND_THREADS)
 k_cache_bounds(const CacheView c, const Ragged r, const int32_t* __restrict__ rep_cnt) {
     __shared__ uint4 part[2][BND_THREADS];
-    grid_dep_wait();
-    grid_dep_launch_next();
     const int lane = threadIdx.x & 31, head = blockIdx.y;
     int left = blockIdx.x, page = -1, live = 0;
     for (int b0 = 0; b0 < r.B; b0 += 32) {
@@ -316,6 +314,9 @@ k_cache_bounds(const CacheView c, const Ragged r, const int32_t* __restrict__ re
         }
         left -= __shfl_sync(0xffffffffu, sum, 31);
     }
+    // which page it is, is written in what was there before the append began; its keys are the append's
+    grid_dep_wait();
+    grid_dep_launch_next();
     if (page < 0 || page >= c.n_pages) return;      // (the append has flagged a page that the table does not name)
     const int ps = 1 << c.shift, nvec = c.d >> 3;
     live = min(live, ps);

@@ -217,34 +217,43 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
     grid_dep_launch_next();
     if (warp == 0) {
         // every CTA's first unit: units of all sequences, 32 at a time (a lane adds up the items of its own)
-        auto units_of = [&](int b) {
+        auto units_of = [&](int b, int& items) {
+            items = 0;
             if (b >= r.B) return 0;
             int o;
             const int n = seq_rows(r, b, o), len = seq_len(r, c, b);
             if (blockIdx.x == 0 && n > j.max_new) atomicOr(status, ST_BAD_COUNT);
-            const int P = ChunkWork::items(n, tq, j.max_new, j.few);
+            const int P = items = ChunkWork::items(n, tq, j.max_new, j.few);
             int u = 0;
             for (int p = 0; p < P; ++p) u += ChunkWork::units(n, len, p, tq, j.causal);
             return u;
         };
-        long long U = 0;
+        long long U = 0, I = 0;                    // units, items (both of one key head)
         int first = 0;
         for (int b0 = 0; b0 < r.B; b0 += 32) {
-            const int u = units_of(b0 + lane);
+            int items;
+            const int u = units_of(b0 + lane, items);
             if (b0 == 0) first = u;
-            unsigned long long x = (unsigned long long)u;
+            unsigned long long x = (unsigned long long)u, y = (unsigned long long)items;
 #pragma unroll
-            for (int m = 16; m > 0; m >>= 1) x += __shfl_xor_sync(0xffffffffu, x, m);
-            U += (long long)x;
+            for (int m = 16; m > 0; m >>= 1) {
+                x += __shfl_xor_sync(0xffffffffu, x, m);
+                y += __shfl_xor_sync(0xffffffffu, y, m);
+            }
+            U += (long long)x; I += (long long)y;
         }
+        // An equal run for every CTA, but not so short that joining an item's shares (about as long as a unit each, one
+        // after the other) takes longer than the units saved: n units in runs of m cost m + n / m, least at sqrt(n).
+        const float share = I > 0 ? sqrtf((float)U / (float)I) : 1.f;
         U *= c.h_kv;
-        const long long per = max((U + gridDim.x - 1) / gridDim.x, 1ll);
+        const long long per = max((U + gridDim.x - 1) / gridDim.x, (long long)max(share, 1.f));
         const long long at = min(per * blockIdx.x, U), end = min(at + per, U);
         int b = 0, p = 0, head = 0, ku = 0;
         long long before = 0;
         if (at < end)
             for (int b0 = 0; b0 < r.B; b0 += 32) {
-                const int own = b0 == 0 ? first : units_of(b0 + lane);
+                int items;
+                const int own = b0 == 0 ? first : units_of(b0 + lane, items);
                 long long sum = own;
 #pragma unroll
                 for (int m = 1; m < 32; m <<= 1) {
@@ -546,7 +555,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                             }
                     }
                 }
-            } else {
+            } else if (__any_sync(0xffffffffu, live)) {
                 // a share of an item: unnormalised, four columns of a row together (a warp's lanes write next to each other)
                 auto part = [&](int piece) { return ws + (2 * (int64_t)(it.c0 + piece) + (piece == 0 ? 1 : 0)) * PART_FLOATS; };
                 const int at = t * 128 + i;
@@ -583,7 +592,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     for (int p = 0; p < it.pieces; ++p)
                         L = fmaf(__ldcg(part(p) + 128 * 256 + 256 + at), ex2_approx(__ldcg(part(p) + 128 * 256 + at) - Mr), L);
                     const float f = L > 0.f ? 1.0f / L : 0.f;
-                    // 32 columns of a piece in flight; the own piece's are still in TMEM, the same numbers
+                    // 32 columns of two pieces in flight
 #pragma unroll 1
                     for (int q = 0; q < NDB * 2; ++q) {
                         if (q * 32 >= c.d) break;
@@ -591,29 +600,21 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
 #pragma unroll
                         for (int e = 0; e < 32; ++e) y[e] = 0.f;
 #pragma unroll 1
-                        for (int p = 0; p < it.pieces; ++p) {
-                            float4 z[8];
-                            if (p == it.piece) {
-                                unsigned x[32];
-                                if (nt > 0) { tmem_ld32_issue(t_o + q * 32, x); tmem_ld_wait(x); }
-                                else {
+                        for (int p = 0; p < it.pieces; p += 2) {
+                            const int p1 = min(p + 1, it.pieces - 1);        // (p itself once more: with a factor of 0)
+                            const float4* o0 = reinterpret_cast<const float4*>(part(p)) + q * 8 * 256 + at;
+                            const float4* o1 = reinterpret_cast<const float4*>(part(p1)) + q * 8 * 256 + at;
+                            float4 z0[8], z1[8];
 #pragma unroll
-                                    for (int e = 0; e < 32; ++e) x[e] = 0u;
-                                }
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    z[e] = make_float4(__uint_as_float(x[4 * e]), __uint_as_float(x[4 * e + 1]),
-                                                       __uint_as_float(x[4 * e + 2]), __uint_as_float(x[4 * e + 3]));
-                            } else {
-                                const float4* o = reinterpret_cast<const float4*>(part(p)) + q * 8 * 256 + at;
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) z[e] = __ldcg(o + e * 256);
-                            }
-                            const float fp = ex2_approx((p == it.piece ? m : __ldcg(part(p) + 128 * 256 + at)) - Mr);
+                            for (int e = 0; e < 8; ++e) { z0[e] = __ldcg(o0 + e * 256); z1[e] = __ldcg(o1 + e * 256); }
+                            const float f0 = ex2_approx(__ldcg(part(p) + 128 * 256 + at) - Mr);
+                            const float f1 = p1 > p ? ex2_approx(__ldcg(part(p1) + 128 * 256 + at) - Mr) : 0.f;
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
-                                y[4 * e] = fmaf(z[e].x, fp, y[4 * e]); y[4 * e + 1] = fmaf(z[e].y, fp, y[4 * e + 1]);
-                                y[4 * e + 2] = fmaf(z[e].z, fp, y[4 * e + 2]); y[4 * e + 3] = fmaf(z[e].w, fp, y[4 * e + 3]);
+                                y[4 * e] = fmaf(z1[e].x, f1, fmaf(z0[e].x, f0, y[4 * e]));
+                                y[4 * e + 1] = fmaf(z1[e].y, f1, fmaf(z0[e].y, f0, y[4 * e + 1]));
+                                y[4 * e + 2] = fmaf(z1[e].z, f1, fmaf(z0[e].z, f0, y[4 * e + 2]));
+                                y[4 * e + 3] = fmaf(z1[e].w, f1, fmaf(z0[e].w, f0, y[4 * e + 3]));
                             }
                         }
                         if (live) {
