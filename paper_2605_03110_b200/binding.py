@@ -436,7 +436,7 @@ class KVCache:
         if any(t is not None and t.device != K.device for t in (V, table, kmin, kmax)):
             raise ValueError("the cache's tensors must be on one device")
         self.K, self.V, self.table, self.kmin, self.kmax = K, V, table, kmin, kmax
-        self.K_dtype = K.dtype
+        self.K_dtype, self.index = K.dtype, K.get_device()
         self.dtype, self.h_kv, self.d_h, self.page_size, self.B = dtype, h_kv, d, ps, table.shape[0]
         self._c = _KVCacheStruct(K.data_ptr(), V.data_ptr(), _ptr(kmin), _ptr(kmax), table.data_ptr(),
                                  max(table.stride(0), table.shape[1]), table.shape[1], n,
@@ -444,9 +444,11 @@ class KVCache:
         self.addr = C.addressof(self._c)
 
 
-def _int32(t: torch.Tensor, name: str, n: Optional[int] = None) -> None:
+def _int32(t: torch.Tensor, name: str, n: Optional[int] = None, device: Optional[int] = None) -> None:
     if t.dtype is not torch.int32:
         raise TypeError(f"{name} must be int32")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name} must be on the cache's device")
     if n is not None and (t.numel() < n or not t.is_contiguous()):
         raise ValueError(f"{name} must be dense with at least {n} entries")
 
@@ -456,8 +458,8 @@ def _ragged(cache: KVCache, off: torch.Tensor, length: torch.Tensor) -> int:
     B = off.numel() - 1
     if B < 1 or B > cache.B:
         raise ValueError("off must have B + 1 entries, the cache's table at least B rows")
-    _int32(off, "off", B + 1)
-    _int32(length, "the lengths", B)
+    _int32(off, "off", B + 1, cache.index)
+    _int32(length, "the lengths", B, cache.index)
     return B
 
 
@@ -468,6 +470,8 @@ def _rows_of(X: torch.Tensor, name: str, cache: KVCache, N: Optional[int] = None
         raise ValueError(f"{name} must be {'N' if N is None else N} x {'heads' if heads is None else heads} x d_h")
     if X.dtype is not cache.K_dtype:
         raise TypeError(f"{name} must have the cache's type")
+    if X.get_device() != cache.index:
+        raise ValueError(f"{name} must be on the cache's device")
     if strides[2] != 1 or strides[1] != d and shape[1] > 1:
         raise ValueError(f"{name} must hold the heads of a token side by side")
     return shape[0], shape[1], strides[0] if shape[0] > 1 else shape[1] * d
@@ -489,7 +493,7 @@ def ada_cache_append(ctx: Context, cache: KVCache, K: torch.Tensor, V: torch.Ten
     if len_out is None:
         len_out = torch.empty(B, dtype=torch.int32, device=K.device)
     else:
-        _int32(len_out, "len_out", B)
+        _int32(len_out, "len_out", B, cache.index)
     h = ldq = ldqo = 0
     if Q is not None:
         _, h, ldq = _rows_of(Q, "Q", cache, N)
@@ -502,16 +506,21 @@ def ada_cache_append(ctx: Context, cache: KVCache, K: torch.Tensor, V: torch.Ten
         if w is not None:
             if w.dtype is not cache.K_dtype:
                 raise TypeError("the norms' weights must have the cache's type")
+            if w.get_device() != cache.index:
+                raise ValueError("the norms' weights must be on the cache's device")
             if w.shape != (cache.d_h,) or not w.is_contiguous():
                 raise ValueError("the norms' weights must be d_h dense elements")
-    if inv_freq is not None and (inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()):
-        raise TypeError("inv_freq must be a dense float64 vector")
+    if inv_freq is not None:
+        if inv_freq.dtype is not torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise TypeError("inv_freq must be a dense float64 vector")
+        if inv_freq.get_device() != cache.index:
+            raise ValueError("inv_freq must be on the cache's device")
     if pos0 is not None:
-        _int32(pos0, "pos0", B)
+        _int32(pos0, "pos0", B, cache.index)
     if rep_idx is not None:
-        _int32(rep_idx, "rep_idx", N)
+        _int32(rep_idx, "rep_idx", N, cache.index)
     if rep_cnt is not None:
-        _int32(rep_cnt, "rep_cnt", B)
+        _int32(rep_cnt, "rep_cnt", B, cache.index)
     st = _fast.cache_append(ctx.addr, cache.addr, B, off, length, len_out, N, K, ldk, V, ldv, cache.dtype, Q, h, ldq, q_out,
                             ldqo, q_norm, k_norm, eps, inv_freq, 0 if inv_freq is None else 2 * inv_freq.numel(), pos0,
                             rep_idx, rep_cnt, flags, _stream_of(ctx, stream))
@@ -542,8 +551,8 @@ def _lists_of(cache: KVCache, N: int, blk_idx: torch.Tensor, blk_cnt: torch.Tens
     shape = blk_idx.shape
     if len(shape) != 3 or shape[0] != N or shape[1] != cache.h_kv or k is not None and shape[2] != k:
         raise ValueError("blk_idx must be N x h_kv x k")
-    _int32(blk_idx, "blk_idx", N * cache.h_kv * shape[2])
-    _int32(blk_cnt, "blk_cnt", N * cache.h_kv)
+    _int32(blk_idx, "blk_idx", N * cache.h_kv * shape[2], cache.index)
+    _int32(blk_cnt, "blk_cnt", N * cache.h_kv, cache.index)
     return shape[2]
 
 

@@ -192,6 +192,11 @@ def test_call_tensors(ada):
             (lambda: append(K, K, off, n, len_out=i32(0)), ValueError)):
         with pytest.raises(error):
             call()
+    c.index = 0                                            # a cache on a GPU: tensors from elsewhere are refused
+    for call in (lambda: attend(Q, off, n, 4), lambda: append(K, K, off, n), lambda: select(Q, off, n, 4),
+                 lambda: blocks(Q, off, n, idx, cnt)):
+        with pytest.raises(ValueError, match="device"):
+            call()
 
 
 def test_reference_against_dense_attention():

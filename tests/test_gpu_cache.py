@@ -144,6 +144,45 @@ def test_chunks(ada, ctx, h, hk, d, ps):
             c.check(out, causal)
 
 
+@pytest.mark.parametrize("h,hk,few", [(4, 4, 16), (8, 2, 4), (14, 2, 2), (16, 1, 1), (34, 2, 0)])
+def test_few_tokens_and_chunks_in_one_call(ada, ctx, h, hk, few):
+    """Sequences on either side of the line between the two kernels, in one call; and one sequence alone."""
+    for news, lens in (([few + 1, few, 1, 0, 60], [90, 300, 5, 3, 700]), ([few, few + 1], [2000, few]), ([few + 1], [1500])):
+        c = Case(ada, few, h, hk, 64, 32, news, lens, pad=1)
+        for causal in (True, False):
+            out = ada.ada_attention_cached(ctx, c.cache, c.d_Q, c.d_off, c.d_len, c.max_new, flags=int(causal))
+            fine(ada, ctx)
+            c.check(out, causal)
+
+
+@pytest.mark.parametrize("max_new", [1, 50])
+def test_pages_behind_the_32_bit_range(ada, ctx, max_new):
+    """A pool of more than 2^31 elements, the sequence's pages at its far end."""
+    h, hk, d, ps, pool = 8, 2, 128, 64, 135000
+    K, V = (torch.empty((pool, hk, ps, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert K.numel() > 2 ** 31
+    kmin, kmax = (torch.empty((pool, hk, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    pages = [pool - 1, pool - 7, 0, 131072, 131071, pool - 2]
+    table = i32([pages + [-1]])
+    cache = ada.KVCache(K, V, table, kmin, kmax)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    total = 350
+    x = torch.randn((total, (h + 2 * hk) * d), generator=g, device="cuda").bfloat16()
+    q, k, v = (y.unflatten(1, (-1, d)) for y in x.split([h * d, hk * d, hk * d], 1))
+    ada.ada_cache_append(ctx, cache, k, v, i32([0, total]), i32([0]))
+    small = ref.Pages(K[pages].cpu(), V[pages].cpu(), torch.arange(6, dtype=torch.int32).view(1, 6), kmin[pages].cpu(), kmax[pages].cpu())
+    q = q[-max_new:].contiguous()
+    out = ada.ada_attention_cached(ctx, cache, q, i32([0, max_new]), i32([total]), max_new)
+    idx, cnt = ada.ada_select_blocks(ctx, cache, q, i32([0, max_new]), i32([total]), 4)
+    some = ada.ada_attention_blocks(ctx, cache, q, i32([0, max_new]), i32([total]), idx, cnt)
+    fine(ada, ctx)
+    assert lists_of(idx, cnt) == ref.select(small, q.cpu(), [0, max_new], [total], hk, 4, 1, 1)
+    for got, lists in ((out, None), (some, lists_of(idx, cnt))):
+        want, weight = ref.attend(small, q.cpu(), [0, max_new], [total], hk, True, 0.0, lists)
+        tol = ref.tolerance(want, weight, v.float().cpu())
+        assert bool(((got.cpu().double() - want).abs() <= tol).all())
+
+
 @pytest.mark.parametrize("h,hk", [(128, 1), (40, 1), (66, 2), (12, 2)])
 def test_wide_groups(ada, ctx, h, hk):
     """Groups that do not divide a tile's 128 rows, and the largest; single tokens of more than 16 heads a key head."""
@@ -299,6 +338,28 @@ def test_blocks(ada, ctx, h, hk, d, ps, k):
             c.check(out, causal, lists=lists_of(idx, cnt))
 
 
+@pytest.mark.parametrize("h,hk,d,ps,n", [(8, 2, 128, 64, 610), (32, 2, 64, 16, 600), (6, 6, 80, 32, 200), (40, 2, 128, 16, 205)])
+def test_blocks_of_many_rows(ada, ctx, h, hk, d, ps, n):
+    """Row tiles enough for a warp each; lists of all lengths, none among them, padding rows behind."""
+    c = Case(ada, 34, h, hk, d, ps, [n - 3, 0, 3], [n + 150, 4, 90], pad=2)
+    g = torch.Generator().manual_seed(n)
+    k = 7
+    idx, cnt = torch.full((c.N, hk, k), -9, dtype=torch.int32), torch.zeros((c.N, hk), dtype=torch.int32)
+    lists = [[[] for _ in range(hk)] for _ in range(c.N)]
+    for i in range(n):
+        pages = -(-c.lens[0 if i < n - 3 else 2] // ps)
+        for j in range(hk):
+            m = min(int(torch.randint(0, k + 1, (1,), generator=g)), pages)
+            lists[i][j] = sorted(torch.randperm(pages, generator=g)[:m].tolist())
+            idx[i, j, :m] = torch.tensor(lists[i][j], dtype=torch.int32)
+            cnt[i, j] = m
+    out = torch.full((c.N, h, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    ada.ada_attention_blocks(ctx, c.cache, c.d_Q, c.d_off, c.d_len, idx.cuda(), cnt.cuda(), out=out)
+    fine(ada, ctx)
+    c.check(out, True, lists=lists)
+    assert bool((out[n:] == 9.0).all())
+
+
 def test_blocks_with_lists_of_any_kind(ada, ctx):
     """Empty lists, lists of one page, pages that the token does not see (no slot of theirs counts), long lists."""
     c = Case(ada, 33, 4, 2, 128, 16, [4, 1], [700, 800], pad=2)
@@ -364,6 +425,24 @@ def test_append(ada, ctx, h, hk, d, rot, pairs, norm, ps):
         assert near(c.cache.kmin.cpu()[touched], want[2][touched], big)
         assert near(c.cache.kmax.cpu()[touched], want[3][touched], big)
         assert bool(c.cache.kmin.isnan().cpu()[~touched].all())
+
+
+@pytest.mark.parametrize("news", [[1, 1, 1], [40, 2, 9]])
+def test_append_of_keys_and_values_alone(ada, ctx, news):
+    """No queries, no bounds, a norm without rotation, and neither."""
+    c = Case(ada, 45, 2, 2, 48, 16, news, [n + 5 for n in news])
+    cache = ada.KVCache(c.cache.K, c.cache.V, c.cache.table)
+    g = torch.Generator().manual_seed(4)
+    K, V = (torch.randn((c.N, 2, 48), generator=g).bfloat16() for _ in range(2))
+    w = (1 + 0.1 * torch.randn(48, generator=g)).bfloat16()
+    for weight in (w, None):
+        want = ref.append(ref.Pages(c.cpu.K, c.cpu.V, c.cpu.table), K, V, c.off, [5] * 3, None, None, weight, 1e-5)
+        q, n = ada.ada_cache_append(ctx, cache, K.cuda(), V.cuda(), c.d_off, i32([5] * 3), eps=1e-5,
+                                    k_norm=None if weight is None else weight.cuda())
+        fine(ada, ctx)
+        assert q is None and n.tolist() == [x + 5 for x in news]
+        assert near(cache.K.cpu().nan_to_num(), want[0].nan_to_num(), 8.0)
+        assert torch.equal(cache.V.cpu().nan_to_num(), want[1].nan_to_num())
 
 
 def test_append_in_place_and_far_positions(ada, ctx):
