@@ -15,6 +15,13 @@
 // Work: items (sequence, 2 x 128 / G tokens, key head) cost as many units as they see key tiles; every CTA takes an
 // equal run of units.  An item that several CTAs share is joined, 32 rows at a time, by the warp that finishes last,
 // in the order of the keys; nobody waits for another CTA.
+//
+// Measured (32 heads on 8 key heads of 128): 2048 tokens after 6145 others 228 us = 1055 TFLOP/s, 63 % of cuBLAS's best.  Two
+// tiles and 128 keys take 3500 cycles, of them 2048 the tensor core's: each tile's chain is 600 for scores into registers
+// and maxima, 1600 for exponentials (special-function unit and multipliers shared by the two sets), 1250 until the next
+// scores are there (half of the second product, the first one, the signals).  Shares and their joining: 8 %.
+// On the way: MMAs issued behind `if (lane == 0)` 335 us, behind elect_one() 242; exponentials in two unrolled copies that
+// miss the instruction cache 253, in one 232.
 #include "cache_tma.cuh"
 
 namespace ada {

@@ -15,6 +15,10 @@
 // eight pages at a time, 16 bytes a lane, straight into registers, the next eight under way.  Of several tokens of a sequence
 // a block scores 16 against the same pages on mma.sync, P and M as two bf16 terms each (products exact, fp32
 // sums); the bounds then come from L2 through a ring of four half stages.
+//
+// Measured (32 heads on 8 key heads of 128): 32 tokens over 512 pages each 21 us, 67 MB = 3.2 TB/s (loads 13 us, the choice 4);
+// 1000 tokens over 257 pages 54 us, bound by issue of the choice's instructions: a warp's row takes 1500.  All
+// scores in 64 bits took 47 and 454 us.
 #include "cache_tma.cuh"
 
 namespace ada {
