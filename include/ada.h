@@ -299,11 +299,11 @@ ada_status ada_attention_reps(ada_ctx* ctx, const void* Q, const void* K, const 
  *     ADA_ERR_UNSUPPORTED, as for ada_attention_reps.
  *   - page_size 16, 32, 64 or 128; d_h a multiple of 16, at most 128; page_stride a multiple of 8, at least
  *     h_kv * page_size * d_h; K, V, kmin, kmax 16-byte aligned; h_kv <= 4096: else ADA_ERR_UNSUPPORTED.
- *   - max_pages: entries of a sequence's table row (max_pages * page_size < 2^30).
+ *   - max_pages: entries of a sequence's table row (max_pages * page_size < 2^30); B <= 2^20, N <= 2^28 rows.
  *
  * The new tokens of all sequences stand one after the other (ragged): sequence b has rows off[b] .. off[b+1] - 1 of
  * every per-token array, off[0] = 0 <= off[1] <= .. <= off[B] <= N (device, B + 1 entries; a sequence may have none).
- * Rows from off[B] on are padding: nothing of them is read or written.  len[b] (device) counts the sequence's tokens in
+ * Rows from off[B] on are padding: they have no influence and are not written.  len[b] (device) counts the sequence's tokens in
  * the cache.  Both are read on the device: nothing returns to the host between calls.
  * Rows of queries hold the heads of a token side by side (head i at i * d_h), rows `ld` elements apart, ld a
  * multiple of 8, 16-byte aligned: columns of a wider projection will do.  Head i reads key head i / (h / h_kv); h is a
@@ -336,7 +336,7 @@ typedef struct {
  *            an ascending list of indices within the sequence's new tokens (for sequences of one length T that is the
  *            layout of ada_select_full and ada_cascade_step).  Each keeps the position that it has in the
  *            sequence; Q is not affected
- *   len_out  optional, DEVICE int32[B], not `len` itself: the sequences' new lengths
+ *   len_out  optional, DEVICE int32[B], overlapping none of the int32 inputs: the sequences' new lengths
  * Arithmetic in fp32, one rounding to bf16.  kmin and kmax of every page written are formed anew from the page's keys
  * below the new length.  Tokens that the table has no room for are dropped (ADA_ERR_BAD_INDEX_SET).  No page that the
  * call writes to may belong to two sequences.
@@ -357,7 +357,8 @@ ada_status ada_cache_append(ada_ctx* ctx, const ada_kv_cache* cache, int64_t B, 
  *   flags    ADA_ATTN_CAUSAL: the sequence's new tokens are its last ones, and each sees the slots up to its own;
  *            0: each sees all len[b] slots
  *   scale    of the scores; 0: 1 / sqrt(d_h).  Not negative
- *   out      bf16, rows of h heads.  A token that sees no slot gets zeros
+ *   out      bf16, rows of h heads; may be Q itself (then ldo = ldq).  A token that sees no slot gets zeros; one that sees
+ *            a NaN, or whose scores leave the range of fp32, gets NaN
  * Scores, softmax statistics and sums in fp32; the probabilities are rounded to bf16 for the second product.
  * The first call on a context allocates its workspace (40 MB): make it before capturing into a CUDA graph.
  */

@@ -61,7 +61,7 @@ ada_status ada_cache_append(ada_ctx* ctx, const ada_kv_cache* cache, int64_t B, 
     Ragged r;
     ada_status st = open_cache(ctx, cache, B, off, len, N, dt, &c, &r);
     if (st != ADA_OK) return st;
-    if ((st = check_append(cache, len, len_out, K, ldk, V, ldv, Q, h, ldq, q_out, ldqo, q_norm, k_norm, eps, inv_freq, rot,
+    if ((st = check_append(cache, B, off, len, N, len_out, pos0, K, ldk, V, ldv, Q, h, ldq, q_out, ldqo, q_norm, k_norm, eps, inv_freq, rot,
                            rep_idx, rep_cnt, flags)) != ADA_OK)
         return st;
     AppendJob j;
@@ -85,7 +85,9 @@ ada_status ada_attention_cached(ada_ctx* ctx, const ada_kv_cache* cache, int64_t
     Ragged r;
     ada_status st = open_cache(ctx, cache, B, off, len, N, dt, &c, &r);
     if (st != ADA_OK || (st = check_heads(cache, h)) != ADA_OK) return st;
-    if ((st = check_rows(Q, h, c.d, ldq)) != ADA_OK || (st = check_rows(out, h, c.d, ldo)) != ADA_OK) return st;
+    if ((st = check_rows(Q, h, c.d, ldq)) != ADA_OK || (st = check_rows(out, h, c.d, ldo)) != ADA_OK ||
+        (st = check_out(Q, ldq, out, ldo)) != ADA_OK)
+        return st;
     if ((flags & ~ADA_ATTN_CAUSAL) != 0 || max_new < 1 || !scale_ok(scale)) return ADA_ERR_INVALID_ARG;
     AttendJob j;
     j.scale = score_scale(scale, c.d);
@@ -139,7 +141,9 @@ ada_status ada_attention_blocks(ada_ctx* ctx, const ada_kv_cache* cache, int64_t
     Ragged r;
     ada_status st = open_cache(ctx, cache, B, off, len, N, dt, &c, &r);
     if (st != ADA_OK || (st = check_heads(cache, h)) != ADA_OK) return st;
-    if ((st = check_rows(Q, h, c.d, ldq)) != ADA_OK || (st = check_rows(out, h, c.d, ldo)) != ADA_OK) return st;
+    if ((st = check_rows(Q, h, c.d, ldq)) != ADA_OK || (st = check_rows(out, h, c.d, ldo)) != ADA_OK ||
+        (st = check_out(Q, ldq, out, ldo)) != ADA_OK)
+        return st;
     if (blk_idx == nullptr || blk_cnt == nullptr || (flags & ~ADA_ATTN_CAUSAL) != 0 || k < 1 || !scale_ok(scale))
         return ADA_ERR_INVALID_ARG;
     if (k > SELECT_MAX_PAGES) return ADA_ERR_UNSUPPORTED;

@@ -60,18 +60,33 @@ inline ada_status check_heads(const ada_kv_cache* kv, int64_t h) {
 // scale of the scores (0: 1 / sqrt(d_h)) is one
 inline bool scale_ok(double scale) { return scale >= 0.0 && scale <= 1e30; }   // also rejects NaN
 
-inline ada_status check_append(const ada_kv_cache* kv, const int32_t* len, const int32_t* len_out, const void* K, int64_t ldk,
+// where the results of an attention call go: apart from the queries, or over them row by row (a row is read before it is written)
+inline ada_status check_out(const void* Q, int64_t ldq, const void* out, int64_t ldo) {
+    return out == Q && ldo != ldq ? ADA_ERR_INVALID_ARG : ADA_OK;
+}
+
+// int32 arrays of na and nb entries have none in common (b may be NULL)
+inline bool apart(const int32_t* a, int64_t na, const int32_t* b, int64_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return b == nullptr || x + (uintptr_t)na * 4 <= y || y + (uintptr_t)nb * 4 <= x;
+}
+
+inline ada_status check_append(const ada_kv_cache* kv, int64_t B, const int32_t* off, const int32_t* len, int64_t N,
+                               const int32_t* len_out, const int32_t* pos0, const void* K, int64_t ldk,
                                const void* V, int64_t ldv, const void* Q, int64_t h, int64_t ldq, const void* q_out,
                                int64_t ldqo, const void* q_norm, const void* k_norm, double eps, const double* inv_freq,
                                int64_t rot, const int32_t* rep_idx, const int32_t* rep_cnt, uint32_t flags) {
     ada_status st;
     if ((st = check_rows(K, kv->h_kv, kv->d_h, ldk)) != ADA_OK || (st = check_rows(V, kv->h_kv, kv->d_h, ldv)) != ADA_OK)
         return st;
-    if ((flags & ~ADA_ROPE_PAIRS) != 0 || len_out == len || (rep_idx == nullptr) != (rep_cnt == nullptr))
+    if ((flags & ~ADA_ROPE_PAIRS) != 0 || (rep_idx == nullptr) != (rep_cnt == nullptr)) return ADA_ERR_INVALID_ARG;
+    // the new lengths are written while other blocks still read these
+    if (len_out != nullptr && !(apart(len_out, B, len, B) && apart(len_out, B, off, B + 1) && apart(len_out, B, pos0, B) &&
+                                apart(len_out, B, rep_cnt, B) && apart(len_out, B, rep_idx, N)))
         return ADA_ERR_INVALID_ARG;
     if (Q != nullptr) {
         if ((st = check_rows(Q, h, kv->d_h, ldq)) != ADA_OK || (st = check_rows(q_out, h, kv->d_h, ldqo)) != ADA_OK) return st;
-        if (q_out == Q && ldqo != ldq) return ADA_ERR_INVALID_ARG;    // a row would overwrite another before it is read
+        if ((st = check_out(Q, ldq, q_out, ldqo)) != ADA_OK) return st;
     } else if (q_out != nullptr || q_norm != nullptr) {
         return ADA_ERR_INVALID_ARG;
     }

@@ -117,9 +117,9 @@ struct ChunkWork {
     static __device__ __forceinline__ int tiles_of(const Item& it, int t) { return max(min(it.units[t] - it.ku, it.take), 0); }
 };
 
-__device__ __forceinline__ float max3(float a, unsigned b, unsigned c) {
+__device__ __forceinline__ float max3(float a, unsigned b, unsigned c) {      // NaN if one of them is
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
     return d;
 }
 __device__ __forceinline__ unsigned long long pack2(float a, float b) {
@@ -226,20 +226,20 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
         // every CTA's first unit: units of all sequences, 32 at a time (a lane adds up the items of its own)
         auto units_of = [&](int b, int& items) {
             items = 0;
-            if (b >= r.B) return 0;
+            long long u = 0;
+            if (b >= r.B) return u;
             int o;
             const int n = seq_rows(r, b, o), len = seq_len(r, c, b);
             if (blockIdx.x == 0 && n > j.max_new) atomicOr(status, ST_BAD_COUNT);
             const int P = items = ChunkWork::items(n, tq, j.max_new, j.few);
-            int u = 0;
             for (int p = 0; p < P; ++p) u += ChunkWork::units(n, len, p, tq, j.causal);
             return u;
         };
         long long U = 0, I = 0;                    // units, items (both of one key head)
-        int first = 0;
+        long long first = 0;
         for (int b0 = 0; b0 < r.B; b0 += 32) {
             int items;
-            const int u = units_of(b0 + lane, items);
+            const long long u = units_of(b0 + lane, items);
             if (b0 == 0) first = u;
             unsigned long long x = (unsigned long long)u, y = (unsigned long long)items;
 #pragma unroll
@@ -260,7 +260,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
         if (at < end)
             for (int b0 = 0; b0 < r.B; b0 += 32) {
                 int items;
-                const int own = b0 == 0 ? first : units_of(b0 + lane, items);
+                const long long own = b0 == 0 ? first : units_of(b0 + lane, items);
                 long long sum = own;
 #pragma unroll
                 for (int m = 1; m < 32; m <<= 1) {
@@ -381,7 +381,6 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
             auto issue_s = [&](int t, unsigned slot) {
                 const unsigned a = desc_lo(smem_u32(qs + t * NDB * BLK_BYTES));
                 const unsigned b = desc_lo(smem_u32(ring + (slot % SLOTS) * SLOT_BYTES));
-                
 #pragma unroll
                 for (int q = 0; q < NDB * 4; ++q)
                     umma_ss(tmem_base + t * 128, a + (q >> 2) * (BLK_BYTES >> 4) + 2 * (q & 3), b + (q >> 2) * (BLK_BYTES >> 4) + 2 * (q & 3), idesc_s, q != 0, lead);
@@ -493,7 +492,9 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     mx[2] = max3(mx[2], z[0][e], z[0][e + 1]);
                     mx[3] = max3(mx[3], z[1][e], z[1][e + 1]);
                 }
-                const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * j.scale);
+                const float top = max3(mx[0], __float_as_uint(mx[1]), __float_as_uint(max3(mx[2], __float_as_uint(mx[3]), __float_as_uint(mx[3])))) * j.scale;
+                const float m_new = fmaxf(m, top);
+                if (!(top < INFINITY)) l = NAN;                             // a NaN, or an overflow, that the row sees
                 if (u == 0) {
                     m = m_new;
                 } else {
@@ -539,7 +540,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
             }
             __nv_bfloat16* dst = j.out + (int64_t)(it.row0 + tok_i) * j.ldo + ((int64_t)it.head * G + g) * c.d;
             if (it.pieces == 1) {
-                const float f = l > 0.f ? 1.0f / l : 0.f;
+                const float f = l == 0.f ? 0.f : 1.0f / l;                   // (NaN stays)
 #pragma unroll
                 for (int q = 0; q < NDB * 2; ++q) {
                     unsigned y[32];
@@ -598,7 +599,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     const float Mr = M > -INFINITY ? M : 0.f;
                     for (int p = 0; p < it.pieces; ++p)
                         L = fmaf(__ldcg(part(p) + 128 * 256 + 256 + at), ex2_approx(__ldcg(part(p) + 128 * 256 + at) - Mr), L);
-                    const float f = L > 0.f ? 1.0f / L : 0.f;
+                    const float f = L == 0.f ? 0.f : 1.0f / L;
                     // 32 columns of two pieces in flight
 #pragma unroll 1
                     for (int q = 0; q < NDB * 2; ++q) {

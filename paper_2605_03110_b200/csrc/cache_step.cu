@@ -515,7 +515,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
         if (TEAM == 1) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float f[2] = {l[nt][0] > 0.f ? 1.0f / l[nt][0] : 0.f, l[nt][1] > 0.f ? 1.0f / l[nt][1] : 0.f};
+                const float f[2] = {l[nt][0] == 0.f ? 0.f : 1.0f / l[nt][0], l[nt][1] == 0.f ? 0.f : 1.0f / l[nt][1]};   // (NaN stays)
                 __nv_bfloat16* dst = out_row(nt * 8 + r0);
 #pragma unroll
                 for (int d = 0; d < KS; ++d)
@@ -559,7 +559,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                     x = fmaf(mrg[(q * 8 + rr) * W + col], f, x);
                 }
                 if (s.pieces == 1) {
-                    if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L > 0.f ? x / L : 0.f);
+                    if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L == 0.f ? 0.f : x / L);
                 } else {
                     mine[row * 128 + col] = x;
                     if (col == 0) { mine[2048 + row] = M; mine[2064 + row] = L; }
@@ -589,7 +589,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                         L = fmaf(__ldcg(part + 2064 + row), f, L);
                         x = fmaf(__ldcg(part + row * 128 + col), f, x);
                     }
-                    if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L > 0.f ? x / L : 0.f);
+                    if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L == 0.f ? 0.f : x / L);
                 }
             }
             __syncthreads();

@@ -71,12 +71,12 @@ def test_call_arguments(tmp_path):
     assert(check_heads(&good, 2) == OK && check_heads(&good, 256) == OK && check_heads(&good, 258) == NO);
     assert(check_heads(&good, 0) == BAD && check_heads(&good, 3) == BAD);
     assert(scale_ok(0.0) && scale_ok(1.0) && !scale_ok(-1.0) && !scale_ok(NAN) && !scale_ok(INFINITY));
-    int32_t* out = ints + 4;
+    int32_t *out = ints + 16, *pos = nullptr;
     const double* f = (double*)at;
     auto app = [&](const void* K, int64_t ldk, const void* Q, int64_t h, const void* qo, int64_t ldqo, const void* qn,
                    const void* kn, double eps, const double* fr, int64_t rot, const int32_t* ri, const int32_t* rc,
                    const int32_t* lo, uint32_t fl) {
-        return check_append(&good, ints, lo, K, ldk, at, 256, Q, h, 512, qo, ldqo, qn, kn, eps, fr, rot, ri, rc, fl);
+        return check_append(&good, 3, ints, ints, 7, lo, pos, K, ldk, at, 256, Q, h, 512, qo, ldqo, qn, kn, eps, fr, rot, ri, rc, fl);
     };
     assert(app(at, 256, at, 4, at, 512, at, at, 1e-6, f, 128, ints, ints, out, 1) == OK);
     assert(app(at, 256, nullptr, 0, nullptr, 0, nullptr, at, 0.0, nullptr, 0, nullptr, nullptr, nullptr, 0) == OK);
@@ -95,6 +95,16 @@ def test_call_arguments(tmp_path):
     for (int64_t rot : {2, 8, 40, 120}) assert(app(at, 256, at, 4, at, 512, at, at, 0.0, f, rot, ints, ints, out, 0) == NO);
     assert(app(at, 256, at, 4, at, 512, at, at, 0.0, f, 128, ints, nullptr, out, 0) == BAD);
     assert(app(at, 256, at, 4, at, 512, at, at, 0.0, f, 128, ints, ints, ints, 0) == BAD);      // new lengths over the old
+    // off has 4 entries, lengths, positions and counts 3, the list 7
+    for (int i = -8; i <= 8; ++i) {
+        const int32_t* lo = ints + i;
+        assert((app(at, 256, at, 4, at, 512, at, at, 0.0, f, 128, nullptr, nullptr, lo, 0) == OK) == (i <= -3 || i >= 4));
+        assert((app(at, 256, at, 4, at, 512, at, at, 0.0, f, 128, ints, ints, lo, 0) == OK) == (i <= -3 || i >= 7));
+        pos = ints + 4;
+        assert((app(at, 256, at, 4, at, 512, at, at, 0.0, f, 128, nullptr, nullptr, lo, 0) == OK) == (i <= -3 || i >= 7));
+        pos = nullptr;
+    }
+    assert(check_out(at, 512, at, 512) == OK && check_out(at, 512, at, 520) == BAD && check_out(at, 512, at + 16, 520) == OK);
     assert(app(at, 256, at, 4, at, 512, at, at, 0.0, f, 128, ints, ints, out, 2) == BAD);
     assert(check_select(&good, 4, 1, 1, ints, ints, 1) == OK && check_select(&good, 4, 2, 2, ints, ints, 0) == OK);
     assert(check_select(&good, 4, 3, 2, ints, ints, 0) == BAD && check_select(&good, 0, 0, 0, ints, ints, 0) == BAD);

@@ -230,6 +230,51 @@ def test_scale_and_large_scores(ada, ctx, news):
         assert bool(((out.cpu().double() - ref_out).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("lists", [False, True])
+@pytest.mark.parametrize("n", [1, 3, 90, 700])
+def test_nan_and_infinity_that_a_token_sees(ada, ctx, n, lists):
+    """A NaN in a key gives NaN in the rows that see it, and only there, wherever it lies in a tile; so does a score of
+    +inf; one of -inf has no weight."""
+    length, j = 900, 1
+    c = Case(ada, 21, 4, 2, 128, 32, [n], [length])
+    pages = -(-length // 32)
+    idx = torch.arange(pages, dtype=torch.int32, device="cuda").expand(n, 2, pages).contiguous()
+    cnt = torch.full((n, 2), pages, dtype=torch.int32, device="cuda")
+    seen_from = torch.arange(length - n, length)             # a token's own slot
+    for value in (math.nan, math.inf):
+        for slot in (0, 2, 5, 18, 127, 450, length - 60, length - 1):
+            page, at = int(c.cpu.table[0, slot // 32]), slot % 32
+            c.cache.K.copy_(c.cpu.K)
+            c.cache.K[page, j, at, 7] = value
+            if lists:
+                out = ada.ada_attention_blocks(ctx, c.cache, c.d_Q, c.d_off, c.d_len, idx, cnt)
+            else:
+                out = ada.ada_attention_cached(ctx, c.cache, c.d_Q, c.d_off, c.d_len, n)
+            fine(ada, ctx)
+            bad = (seen_from >= slot).view(-1, 1).expand(n, 4) & (torch.arange(4) // 2 == j)
+            if value == math.inf:
+                bad = bad & (c.Q[:, :, 7] > 0)
+            assert torch.equal(out.cpu().isnan().all(-1), bad), slot
+            assert torch.equal(out.cpu().isnan().any(-1), bad), slot
+            assert bool(out.cpu().isfinite().all(-1)[~bad].all())
+
+
+@pytest.mark.parametrize("news,lens", [([1] * 5, [3, 900, 64, 2000, 1]), ([200], [5000]), ([1, 90, 2, 300], [700, 90, 2, 1000])])
+def test_output_over_the_queries(ada, ctx, news, lens):
+    c = Case(ada, 22, 8, 2, 128, 64, news, lens)
+    out = c.d_Q.clone()
+    assert ada.ada_attention_cached(ctx, c.cache, out, c.d_off, c.d_len, c.max_new, out=out) is out
+    fine(ada, ctx)
+    c.check(out, True)
+    k = 4
+    idx, cnt = ada.ada_select_blocks(ctx, c.cache, c.d_Q, c.d_off, c.d_len, k)
+    apart = ada.ada_attention_blocks(ctx, c.cache, c.d_Q, c.d_off, c.d_len, idx, cnt)
+    over = c.d_Q.clone()
+    ada.ada_attention_blocks(ctx, c.cache, over, c.d_off, c.d_len, idx, cnt, out=over)
+    fine(ada, ctx)
+    assert torch.equal(over, apart)
+
+
 def test_long_sequence_split_over_all_sms(ada, ctx):
     """One row tile of 20000 keys: every SM has a share, joined in the order of the keys; repeated calls agree."""
     c = Case(ada, 10, 4, 1, 64, 128, [1], [20000])
