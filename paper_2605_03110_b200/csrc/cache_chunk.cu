@@ -567,75 +567,93 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 // a share of an item: unnormalised, four columns of a row together (a warp's lanes write next to each other)
                 auto part = [&](int piece) { return ws + (2 * (int64_t)(it.c0 + piece) + (piece == 0 ? 1 : 0)) * PART_FLOATS; };
                 const int at = t * 128 + i;
-                float4* mine = reinterpret_cast<float4*>(part(it.piece)) + at;
-#pragma unroll
-                for (int q = 0; q < NDB * 2; ++q) {
-                    unsigned y[32];
-                    if (nt > 0) { tmem_ld32_issue(t_o + q * 32, y); tmem_ld_wait(y); }
-                    else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) y[e] = 0u;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        __stcg(mine + (q * 8 + e) * 256, make_float4(__uint_as_float(y[4 * e]), __uint_as_float(y[4 * e + 1]),
-                                                                     __uint_as_float(y[4 * e + 2]), __uint_as_float(y[4 * e + 3])));
-                }
-                __stcg(part(it.piece) + 128 * 256 + at, m);
-                __stcg(part(it.piece) + 128 * 256 + 256 + at, l);
-                __threadfence();
-                __syncwarp();
+                unsigned* ctr = counters + ((size_t)it.c1 * 2 + t) * 4 + quad;
+                // the one that comes last joins the shares, its own out of TMEM: where the others are all there already, it
+                // need not be written
                 unsigned last = 0u;
-                if (lane == 0) {
-                    unsigned* ctr = counters + ((size_t)it.c1 * 2 + t) * 4 + quad;
-                    last = atomicAdd(ctr, 1u) + 1u == (unsigned)it.pieces;
-                    if (last) *ctr = 0u;                                     // as the next call finds it
-                }
+                if (lane == 0) last = ld_acquire(ctr) + 1u == (unsigned)it.pieces;
                 last = __shfl_sync(0xffffffffu, last, 0);
-                if (last) {
-                    __threadfence();
-                    float M = -INFINITY, L = 0.f;
-                    for (int p = 0; p < it.pieces; ++p) M = fmaxf(M, __ldcg(part(p) + 128 * 256 + at));
-                    const float Mr = M > -INFINITY ? M : 0.f;
-                    for (int p = 0; p < it.pieces; ++p)
-                        L = fmaf(__ldcg(part(p) + 128 * 256 + 256 + at), ex2_approx(__ldcg(part(p) + 128 * 256 + at) - Mr), L);
-                    const float f = L == 0.f ? 0.f : 1.0f / L;
-                    // 32 columns of two pieces in flight
-#pragma unroll 1
+                if (!last) {
+                    float4* mine = reinterpret_cast<float4*>(part(it.piece)) + at;
+#pragma unroll
                     for (int q = 0; q < NDB * 2; ++q) {
-                        if (q * 32 >= c.d) break;
-                        float y[32];
+                        unsigned y[32];
+                        if (nt > 0) { tmem_ld32_issue(t_o + q * 32, y); tmem_ld_wait(y); }
+                        else {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) y[e] = 0.f;
+                            for (int e = 0; e < 32; ++e) y[e] = 0u;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            __stcg(mine + (q * 8 + e) * 256, make_float4(__uint_as_float(y[4 * e]), __uint_as_float(y[4 * e + 1]),
+                                                                         __uint_as_float(y[4 * e + 2]), __uint_as_float(y[4 * e + 3])));
+                    }
+                    __stcg(part(it.piece) + 128 * 256 + at, m);
+                    __stcg(part(it.piece) + 128 * 256 + 256 + at, l);
+                    __threadfence();
+                    __syncwarp();
+                    if (lane == 0) last = atomicAdd(ctr, 1u) + 1u == (unsigned)it.pieces;
+                    last = __shfl_sync(0xffffffffu, last, 0);
+                }
+                if (last) {
+                    if (lane == 0) *ctr = 0u;                                // as the next call finds it
+                    __threadfence();
+                    float M = m, L = 0.f;
+#pragma unroll 2
+                    for (int p = 0; p < it.pieces; ++p)
+                        if (p != it.piece) M = fmaxf(M, __ldcg(part(p) + 128 * 256 + at));
+                    const float Mr = M > -INFINITY ? M : 0.f;
+#pragma unroll 2
+                    for (int p = 0; p < it.pieces; ++p) {
+                        const bool own = p == it.piece;
+                        L = fmaf(own ? l : __ldcg(part(p) + 128 * 256 + 256 + at),
+                                 ex2_approx((own ? m : __ldcg(part(p) + 128 * 256 + at)) - Mr), L);
+                    }
+                    const float f = L == 0.f ? 0.f : 1.0f / L;
+                    // 64 columns at a time, in the order of the keys whoever joins them
 #pragma unroll 1
-                        for (int p = 0; p < it.pieces; p += 2) {
-                            const int p1 = min(p + 1, it.pieces - 1);        // (p itself once more: with a factor of 0)
-                            const float4* o0 = reinterpret_cast<const float4*>(part(p)) + q * 8 * 256 + at;
-                            const float4* o1 = reinterpret_cast<const float4*>(part(p1)) + q * 8 * 256 + at;
-                            float4 z0[8], z1[8];
+                    for (int q = 0; q < NDB; ++q) {
+                        float y[64];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) { z0[e] = __ldcg(o0 + e * 256); z1[e] = __ldcg(o1 + e * 256); }
-                            const float f0 = ex2_approx(__ldcg(part(p) + 128 * 256 + at) - Mr);
-                            const float f1 = p1 > p ? ex2_approx(__ldcg(part(p1) + 128 * 256 + at) - Mr) : 0.f;
+                        for (int e = 0; e < 64; ++e) y[e] = 0.f;
+#pragma unroll 1
+                        for (int p = 0; p < it.pieces; ++p) {
+                            if (p != it.piece) {
+                                const float4* o = reinterpret_cast<const float4*>(part(p)) + q * 16 * 256 + at;
+                                float4 z[16];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                y[4 * e] = fmaf(z1[e].x, f1, fmaf(z0[e].x, f0, y[4 * e]));
-                                y[4 * e + 1] = fmaf(z1[e].y, f1, fmaf(z0[e].y, f0, y[4 * e + 1]));
-                                y[4 * e + 2] = fmaf(z1[e].z, f1, fmaf(z0[e].z, f0, y[4 * e + 2]));
-                                y[4 * e + 3] = fmaf(z1[e].w, f1, fmaf(z0[e].w, f0, y[4 * e + 3]));
+                                for (int e = 0; e < 16; ++e) z[e] = __ldcg(o + e * 256);
+                                const float fp = ex2_approx(__ldcg(part(p) + 128 * 256 + at) - Mr);
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) {
+                                    y[4 * e] = fmaf(z[e].x, fp, y[4 * e]);
+                                    y[4 * e + 1] = fmaf(z[e].y, fp, y[4 * e + 1]);
+                                    y[4 * e + 2] = fmaf(z[e].z, fp, y[4 * e + 2]);
+                                    y[4 * e + 3] = fmaf(z[e].w, fp, y[4 * e + 3]);
+                                }
+                            } else if (nt > 0) {
+                                const float fp = ex2_approx(m - Mr);
+#pragma unroll
+                                for (int v = 0; v < 2; ++v) {
+                                    unsigned o[32];
+                                    tmem_ld32_issue(t_o + q * 64 + v * 32, o);
+                                    tmem_ld_wait(o);
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e) y[v * 32 + e] = fmaf(__uint_as_float(o[e]), fp, y[v * 32 + e]);
+                                }
                             }
                         }
                         if (live) {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 8)
-                                if (q * 32 + e < c.d) {
+                            for (int e = 0; e < 64; e += 8)
+                                if (q * 64 + e < c.d) {
                                     unsigned w[4];
 #pragma unroll
                                     for (int v = 0; v < 4; ++v) {
                                         const __nv_bfloat162 h = __floats2bfloat162_rn(y[e + 2 * v] * f, y[e + 2 * v + 1] * f);
                                         w[v] = *reinterpret_cast<const unsigned*>(&h);
                                     }
-                                    *reinterpret_cast<uint4*>(dst + q * 32 + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                                    *reinterpret_cast<uint4*>(dst + q * 64 + e) = make_uint4(w[0], w[1], w[2], w[3]);
                                 }
                         }
                     }

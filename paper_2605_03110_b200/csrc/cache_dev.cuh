@@ -87,6 +87,11 @@ static __device__ __forceinline__ void shares_of(int64_t first, int n, int64_t p
     c0 = c - (int)(((unsigned)before + p32 - 1u) / p32);
     c1 = c + (int)(((unsigned)after + p32 - 1u) / p32);
 }
+static __device__ __forceinline__ unsigned ld_acquire(const unsigned* p) {
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
 static __device__ __forceinline__ int64_t slot_at(const CacheView& c, int page, int head, int slot) {
     return (int64_t)page * c.page_stride + ((int64_t)(head << c.shift) + slot) * c.d;
 }
