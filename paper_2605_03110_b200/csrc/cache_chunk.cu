@@ -16,10 +16,11 @@
 // equal run of units.  An item that several CTAs share is joined, 32 rows at a time, by the warp that finishes last,
 // in the order of the keys; nobody waits for another CTA.
 //
-// Measured (32 heads on 8 key heads of 128): 2048 tokens after 6145 others 228 us = 1055 TFLOP/s, 63 % of cuBLAS's best.  Two
+// Measured (32 heads on 8 key heads of 128): 2048 tokens after 6145 others 224 us = 1075 TFLOP/s, 65 % of cuBLAS's best.  Two
 // tiles and 128 keys take 3500 cycles, of them 2048 the tensor core's: each tile's chain is 600 for scores into registers
 // and maxima, 1600 for exponentials (special-function unit and multipliers shared by the two sets), 1250 until the next
-// scores are there (half of the second product, the first one, the signals).  Shares and their joining: 8 %.
+// scores are there (half of the second product, the first one, the signals).  An item's output takes 2.8 us, a share's
+// 3.5, joining two shares 6 (11 before the last one's own came straight out of TMEM: 230 us).
 // On the way: MMAs issued behind `if (lane == 0)` 335 us, behind elect_one() 242; exponentials in two unrolled copies that
 // miss the instruction cache 253, in one 232.
 #include "cache_tma.cuh"
@@ -42,8 +43,8 @@ struct ChunkShared {
     unsigned long long q_full, q_empty, full[10], empty[10], s_full[2], p_full[2][2], o_full[2], o_empty[2];
     unsigned tmem_base;
     int abort_flag[2];
-    int start[4];                                 // b, p, head, ku of the CTA's first unit
-    long long range[3];                           // first unit, one past the last, units per CTA
+    int start[5];                                 // b, p, head, place within the item: where the CTA's run begins; turn
+    long long range[3];                           // first place, one past the last, places per CTA
 };
 template <int NDB> __host__ __device__ constexpr int ch_smem() { return 14 * BLK_BYTES + (int)sizeof(ChunkShared); }
 static_assert(ch_smem<2>() <= 227 * 1024, "shared memory budget");
@@ -61,10 +62,15 @@ struct Item {
     int pieces, piece, c0, c1;
 };
 
-// tq tokens per row tile
+// tq tokens per row tile.  Work is dealt out in places: `turn` of them for an item and one for each of its units behind them; a
+// CTA has the units whose places are in its run.  Where a CTA's run holds several items, an item's queries and output take about
+// as long as CH_TURN units; where items are longer than that, each of their shares has that to do, and turn is 0.
+// (8 sequences of 1 to 517 new tokens, 32 heads: 146 us without, 142 with 2 places, 139 with 3; one of 17 after 3000, in shares:
+// 23.0 without, 24.4 with 3.)
+constexpr int CH_TURN = 3;
 struct ChunkWork {
     long long at, end, per;
-    int b, p, head, ku;
+    int b, p, head, place, turn;          // place: of the item that many are behind
     int n, off, len, nu, P;
 
     static __device__ __forceinline__ int limit(int n, int len, int tok, int causal) {   // keys that the tokens below `tok` see
@@ -84,8 +90,8 @@ struct ChunkWork {
     }
     __device__ __forceinline__ bool next(Item& it, const Ragged& r, const CacheView& c, int tq, int causal, int max_new, int few) {
         if (at >= end) return false;
-        while (P == 0 || ku >= nu) {
-            ku = 0;
+        while (P == 0 || place >= nu + turn) {
+            place = 0;
             if (P == 0 || ++head >= c.h_kv) {
                 head = 0;
                 if (P == 0 || ++p >= P) {
@@ -97,7 +103,12 @@ struct ChunkWork {
                 nu = units(n, len, p, tq, causal);
             }
         }
-        const int t0 = p * 2 * tq;
+        if (place < turn) {
+            at += turn - place;
+            place = turn;
+            if (at >= end) return false;
+        }
+        const int t0 = p * 2 * tq, ku = place - turn;
         it.b = b; it.head = head; it.row0 = off + t0;
         it.n_tok = min(min(n, max_new) - t0, 2 * tq);
         it.first_lim = causal ? len - n + t0 + 1 : len;
@@ -110,7 +121,7 @@ struct ChunkWork {
         shares_of(first, nu, per, blockIdx.x, it.c0, it.c1);
         it.pieces = it.c1 - it.c0 + 1;
         it.piece = (int)blockIdx.x - it.c0;
-        at += it.take; ku += it.take;
+        at += it.take; place += it.take;
         return true;
     }
     // key tiles of row tile t in this CTA's share of the item
@@ -237,10 +248,11 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
         };
         long long U = 0, I = 0;                    // units, items (both of one key head)
         long long first = 0;
+        int first_items = 0;
         for (int b0 = 0; b0 < r.B; b0 += 32) {
             int items;
             const long long u = units_of(b0 + lane, items);
-            if (b0 == 0) first = u;
+            if (b0 == 0) { first = u; first_items = items; }
             unsigned long long x = (unsigned long long)u, y = (unsigned long long)items;
 #pragma unroll
             for (int m = 16; m > 0; m >>= 1) {
@@ -252,15 +264,17 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
         // An equal run for every CTA, but not so short that joining an item's shares (about as long as a unit each, one
         // after the other) takes longer than the units saved: n units in runs of m cost m + n / m, least at sqrt(n).
         const float share = I > 0 ? sqrtf((float)U / (float)I) : 1.f;
-        U *= c.h_kv;
+        const int turn = I * c.h_kv >= (long long)gridDim.x ? CH_TURN : 0;
+        U = (U + turn * I) * c.h_kv;
         const long long per = max((U + gridDim.x - 1) / gridDim.x, (long long)max(share, 1.f));
         const long long at = min(per * blockIdx.x, U), end = min(at + per, U);
-        int b = 0, p = 0, head = 0, ku = 0;
+        int b = 0, p = 0, head = 0, place = 0;
         long long before = 0;
         if (at < end)
             for (int b0 = 0; b0 < r.B; b0 += 32) {
-                int items;
-                const long long own = b0 == 0 ? first : units_of(b0 + lane, items);
+                int items = first_items;
+                long long own = b0 == 0 ? first : units_of(b0 + lane, items);
+                own += turn * items;
                 long long sum = own;
 #pragma unroll
                 for (int m = 1; m < 32; m <<= 1) {
@@ -275,20 +289,20 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                     int o;
                     const int n = seq_rows(r, b, o), len = seq_len(r, c, b);
                     long long rest = at - before * c.h_kv;
-                    int u = ChunkWork::units(n, len, 0, tq, j.causal);
+                    int u = ChunkWork::units(n, len, 0, tq, j.causal) + turn;
                     while (rest >= (long long)u * c.h_kv) {
                         rest -= (long long)u * c.h_kv;
                         ++p;
-                        u = ChunkWork::units(n, len, p, tq, j.causal);
+                        u = ChunkWork::units(n, len, p, tq, j.causal) + turn;
                     }
                     head = (int)(rest / u);
-                    ku = (int)(rest % u);
+                    place = (int)(rest % u);
                     break;
                 }
                 before += __shfl_sync(0xffffffffu, sum, 31);
             }
         if (lane == 0) {
-            sh.start[0] = b; sh.start[1] = p; sh.start[2] = head; sh.start[3] = ku;
+            sh.start[0] = b; sh.start[1] = p; sh.start[2] = head; sh.start[3] = place; sh.start[4] = turn;
             sh.range[0] = at; sh.range[1] = end; sh.range[2] = per;
         }
     } else if (blockIdx.x == 0 && warp == 2) {
@@ -300,7 +314,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
     const unsigned tmem_base = sh.tmem_base;
     ChunkWork work;
     work.at = sh.range[0]; work.end = sh.range[1]; work.per = sh.range[2];
-    work.b = sh.start[0]; work.p = sh.start[1]; work.head = sh.start[2]; work.ku = sh.start[3];
+    work.b = sh.start[0]; work.p = sh.start[1]; work.head = sh.start[2]; work.place = sh.start[3]; work.turn = sh.start[4];
     work.n = work.off = work.len = work.nu = work.P = 0;
     if (work.at < work.end) {
         work.load_seq(r, c, tq, j.max_new, j.few);
