@@ -31,6 +31,7 @@ constexpr int SEL_PAGES = 64;            // pages per stage: eight for every war
 constexpr int SEL_ROWS = 16;             // tokens of a tile
 constexpr int SEL_RING = 4;              // half stages (the maxima or the minima of SEL_PAGES pages) in shared memory
 constexpr int SEL_SPAN = 512;            // scores of a row that one warp counts alone
+constexpr int SEL_LEFT = 64;             // of them left to choose from, room for
 constexpr float SEL_NONE = -3.402823466e38f;   // of pages that do not compete
 // |fp32 score - s(p)| <= (error + (G - 1) 2^-24) sum_e (P_e + |M_e|) a_e, a_e the largest |bound| of element e in any
 // page; P is an fp32 sum over G heads, (G - 1) 2^-24.
@@ -87,6 +88,7 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
     const int rb = sel_row(c.d);
     unsigned char* a_tile = smem + ring_room;                   // [P hi, P lo, M hi, M lo][16][rb]
     float* score = reinterpret_cast<float*>(ONE ? smem : a_tile + 4 * SEL_ROWS * rb);
+    const int left_at = ONE ? stride * 4 : 0;                   // what is left of a row: behind the scores, over the ring
     grid_dep_wait();
     grid_dep_launch_next();
     if (blockIdx.x == 0 && head == 0) check_ragged(r, c, status, tid, SEL_THREADS);
@@ -211,12 +213,17 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
         } else {
             const int nhalf = 2 * ((nb_all + SEL_PAGES - 1) / SEL_PAGES);
             // half stage i: the maxima (i even) or minima (odd) of pages 64 (i / 2) ..; a warp's half has a page, 16 bytes a lane
-            int id = -1;                                         // lane q: the table's entry for the warp's q-th page
+            int id = -1, id_next = -1;                           // lane q: the table's entry for the warp's q-th page
+            auto fetch_ids = [&](int p0) {
+                const int p = p0 + warp * 8 + lane;
+                id_next = lane < 8 && p < nb_all ? page_of(c, b, p, status) : -1;
+            };
+            fetch_ids(0);
             auto load_half = [&](int i) {
                 if (i < nhalf) {
                     if ((i & 1) == 0) {
-                        const int p = (i >> 1) * SEL_PAGES + warp * 8 + lane;
-                        id = lane < 8 && p < nb_all ? page_of(c, b, p, status) : -1;
+                        id = id_next;
+                        fetch_ids(((i >> 1) + 1) * SEL_PAGES);
                     }
                     const __nv_bfloat16* bounds = ((i & 1) ? c.kmin : c.kmax) + (int64_t)head * c.d + v * 8;
                     const unsigned at = tc::smem_u32(smem + (i & (SEL_RING - 1)) * sel_half(c.d)) + (warp * 8) * rb + v * 16;
@@ -378,9 +385,8 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
             continue;
         }
         float* s = score + t * stride;
-        const float4* s4 = reinterpret_cast<const float4*>(s);
         const int first = j.n_first, last = nb - j.n_last;       // pages [first, last) compete for `need` places
-        const int n4 = (nb + 3) >> 2;                            // float4s of the row
+        int n4 = (nb + 3) >> 2;                                  // float4s of the row
         // the others are out of it, and listed without further ado
         for (int p = at0; p < first; p += step) { s[p] = SEL_NONE; idx[p] = p; }
         for (int p = last + at0; p < n4 * 4; p += step) {
@@ -413,47 +419,8 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
             continue;
         }
         const float E = ((ONE ? SEL_ERR_ONE : SEL_ERR_MMA) + (float)G * 6e-8f) * A + 1e-35f;
-        float mn = INFINITY, mx = SEL_NONE;
-        for (int i = at0; i < n4; i += step) {
-            const float4 x = s4[i];
-            mx = fmaxf(mx, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)));
-            mn = fminf(mn, fminf(fminf(x.x == SEL_NONE ? mn : x.x, x.y == SEL_NONE ? mn : x.y), fminf(x.z == SEL_NONE ? mn : x.z, x.w == SEL_NONE ? mn : x.w)));
-        }
-        // at least `need` scores are >= lo, fewer than that > hi (as keys: integers that order as the scores do)
-        unsigned hi = most_of(sort_key(mx)), lo = ~most_of(~sort_key(mn));
-        while (lo < hi) {
-            const unsigned mid = lo + ((hi - lo + 1u) >> 1);
-            const float at = key_value(mid);
-            int ge = 0;
-#pragma unroll 2
-            for (int i = at0; i < n4; i += step) {
-                const float4 x = s4[i];
-                ge += (x.x >= at) + (x.y >= at) + (x.z >= at) + (x.w >= at);
-            }
-            ge = sum_of(ge);
-            if (ge >= need) lo = mid; else hi = mid - 1u;
-            if (ge == need) {                                    // the smallest of them is the one that is sought
-                mn = INFINITY;
-                for (int i = at0; i < n4; i += step) {
-                    const float4 x = s4[i];
-                    mn = fminf(mn, fminf(fminf(x.x >= at ? x.x : mn, x.y >= at ? x.y : mn), fminf(x.z >= at ? x.z : mn, x.w >= at ? x.w : mn)));
-                }
-                lo = ~most_of(~sort_key(mn));
-                break;
-            }
-        }
-        // undecided if below <= s <= above
-        const float kth = key_value(lo), above = __fadd_ru(kth, __fmul_ru(2.0f, E)), below = __fadd_rd(kth, -__fmul_ru(2.0f, E));
-        int in = 0;                                              // certain ones, and 65536 for every undecided one
-        for (int i = at0; i < n4; i += step) {
-            const float4 x = s4[i];
-            in += (x.x > above ? 1 : x.x >= below ? 65536 : 0) + (x.y > above ? 1 : x.y >= below ? 65536 : 0) +
-                  (x.z > above ? 1 : x.z >= below ? 65536 : 0) + (x.w > above ? 1 : x.w >= below ? 65536 : 0);
-        }
-        in = sum_of(in);
-        const int band = in >> 16;
-        need -= in & 0xffff;
         // places of the pages of 32 float4s for which `is` holds, ascending: what a warp writes them with
+        const float4* s4 = reinterpret_cast<const float4*>(s);
         auto list = [&](auto is, auto put) {
             int n_put = 0;
             for (int i0 = 0; i0 < n4; i0 += 32) {
@@ -470,15 +437,126 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
                 for (int e = 0; e < 4; ++e)
                     if (y[e]) put(before++, 4 * (i0 + lane) + e);
             }
+            return n_put;
         };
-        float cut = below;                                       // in the end: in if s >= cut
+        // A warp alone with few places to give first leaves aside what cannot have one: if `need` groups of pages have a score of
+        // at least t0 each, no page below t0 - 2 E matters.  What remains, mostly a few more than `need`, is two a lane.
+        bool left = tw == 1 && need <= 32 && n4 * 4 > SEL_LEFT;
+        float va = SEL_NONE, vb = SEL_NONE;                      // number `lane` and 32 + lane of what remains
+        int pa = 0, pb = 0, n_left = 0;
+        // of the lanes' values (va, vb) the need-th largest, or with `slack` one up to so many places behind it; SEL_NONE if there
+        // are not that many
+        auto kth_of = [&](int slack) {
+            const unsigned ka = sort_key(va), kb = sort_key(vb), none = sort_key(SEL_NONE);
+            unsigned hi = __reduce_max_sync(0xffffffffu, max(ka, kb));
+            unsigned lo = __reduce_min_sync(0xffffffffu, min(ka == none ? ~0u : ka, kb == none ? ~0u : kb));
+            if (__popc(__ballot_sync(0xffffffffu, ka >= lo)) + __popc(__ballot_sync(0xffffffffu, kb >= lo)) < need) return SEL_NONE;
+            while (lo < hi) {
+                const unsigned mid = lo + ((hi - lo + 1u) >> 1);
+                const int ge = __popc(__ballot_sync(0xffffffffu, ka >= mid)) + __popc(__ballot_sync(0xffffffffu, kb >= mid));
+                if (ge >= need) lo = mid; else hi = mid - 1u;
+                if (ge >= need && ge <= need + slack) {          // the smallest of them
+                    lo = __reduce_min_sync(0xffffffffu, min(ka >= mid ? ka : ~0u, kb >= mid ? kb : ~0u));
+                    break;
+                }
+            }
+            return key_value(lo);
+        };
+        if (left) {
+            const int step2 = need > 16 ? 64 : 32;               // groups: 32, or 64 where many places are to be given
+            for (int i = lane; i < n4; i += 64) {
+                const float4 x = s4[i], y = i + 32 < n4 ? s4[i + 32] : make_float4(SEL_NONE, SEL_NONE, SEL_NONE, SEL_NONE);
+                va = fmaxf(va, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)));
+                vb = fmaxf(vb, fmaxf(fmaxf(y.x, y.y), fmaxf(y.z, y.w)));
+            }
+            if (step2 == 32) { va = fmaxf(va, vb); vb = SEL_NONE; }
+            const float t0 = fmaxf(__fadd_rd(kth_of(2), -__fmul_ru(2.0f, E)), -2e36f);    // (SEL_NONE is below)
+            float* room_v = reinterpret_cast<float*>(smem + left_at) + warp * 2 * SEL_LEFT;
+            int* room_p = reinterpret_cast<int*>(room_v + SEL_LEFT);
+            __syncwarp();                                        // (the row before has been read out of it)
+            n_left = list([&](float x) { return x >= t0; }, [&](int at, int p) {
+                if (at < SEL_LEFT) { room_v[at] = s[p]; room_p[at] = p; }
+            });
+            __syncwarp();
+            left = n_left <= SEL_LEFT;
+            if (left) {
+                const bool x = lane < n_left, y = 32 + lane < n_left;
+                va = x ? room_v[lane] : SEL_NONE;
+                vb = y ? room_v[32 + lane] : SEL_NONE;
+                pa = x ? room_p[lane] : 0;
+                pb = y ? room_p[32 + lane] : 0;
+            }
+        }
+        float kth;
+        if (left) {
+            kth = kth_of(0);
+        } else {
+            float mn = INFINITY, mx = SEL_NONE;
+            for (int i = at0; i < n4; i += step) {
+                const float4 x = s4[i];
+                mx = fmaxf(mx, fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)));
+                mn = fminf(mn, fminf(fminf(x.x == SEL_NONE ? mn : x.x, x.y == SEL_NONE ? mn : x.y), fminf(x.z == SEL_NONE ? mn : x.z, x.w == SEL_NONE ? mn : x.w)));
+            }
+            // at least `need` scores are >= lo, fewer than that > hi (as keys: integers that order as the scores do)
+            unsigned hi = most_of(sort_key(mx)), lo = ~most_of(~sort_key(mn));
+            while (lo < hi) {
+                const unsigned mid = lo + ((hi - lo + 1u) >> 1);
+                const float at = key_value(mid);
+                int ge = 0;
+#pragma unroll 2
+                for (int i = at0; i < n4; i += step) {
+                    const float4 x = s4[i];
+                    ge += (x.x >= at) + (x.y >= at) + (x.z >= at) + (x.w >= at);
+                }
+                ge = sum_of(ge);
+                if (ge >= need) lo = mid; else hi = mid - 1u;
+                if (ge == need) {                                // the smallest of them is the one that is sought
+                    mn = INFINITY;
+                    for (int i = at0; i < n4; i += step) {
+                        const float4 x = s4[i];
+                        mn = fminf(mn, fminf(fminf(x.x >= at ? x.x : mn, x.y >= at ? x.y : mn), fminf(x.z >= at ? x.z : mn, x.w >= at ? x.w : mn)));
+                    }
+                    lo = ~most_of(~sort_key(mn));
+                    break;
+                }
+            }
+            kth = key_value(lo);
+        }
+        // undecided if below <= s <= above
+        const float above = __fadd_ru(kth, __fmul_ru(2.0f, E)), below = __fadd_rd(kth, -__fmul_ru(2.0f, E));
+        const unsigned before = (1u << lane) - 1u;
+        unsigned ua = 0u, ub = 0u;                               // undecided ones among what remains
+        int band;
+        if (left) {
+            ua = __ballot_sync(0xffffffffu, va >= below && va <= above);
+            ub = __ballot_sync(0xffffffffu, vb >= below && vb <= above);
+            band = __popc(ua) + __popc(ub);
+            need -= __popc(__ballot_sync(0xffffffffu, va > above)) + __popc(__ballot_sync(0xffffffffu, vb > above));
+        } else {
+            int in = 0;                                          // certain ones, and 65536 for every undecided one
+            for (int i = at0; i < n4; i += step) {
+                const float4 x = s4[i];
+                in += (x.x > above ? 1 : x.x >= below ? 65536 : 0) + (x.y > above ? 1 : x.y >= below ? 65536 : 0) +
+                      (x.z > above ? 1 : x.z >= below ? 65536 : 0) + (x.w > above ? 1 : x.w >= below ? 65536 : 0);
+            }
+            in = sum_of(in);
+            band = in >> 16;
+            need -= in & 0xffff;
+        }
+        const int at_a = __popc(ua & before), at_b = __popc(ua) + __popc(ub & before);   // places among the undecided ones
+        unsigned chosen = 0xffffffffu;                           // of the undecided ones
         if (band != need) {
             if (band > 32) {
                 if (mate == 0 && lane == 0) sh.hard[atomicAdd(&sh.n_hard, 1)] = t;
                 continue;
             }
             // every warp of the team lists them; each scores its share of them in 64 bits
-            list([&](float x) { return x >= below && x <= above; }, [&](int at, int p) { sh.list[warp][at] = p; });
+            if (left) {
+                if (ua >> lane & 1u) sh.list[warp][at_a] = pa;
+                if (ub >> lane & 1u) sh.list[warp][at_b] = pb;
+            } else {
+                list([&](float x) { return x >= below && x <= above; }, [&](int at, int p) { sh.list[warp][at] = p; });
+            }
             __syncwarp();
             const int mine = lane < band ? sh.list[warp][lane] : INT_MAX;
             const int page_l = lane < band ? page_of(c, b, mine, status) : -1;
@@ -486,8 +564,9 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
             const bool on = lane * 4 < c.d;
 #pragma unroll
             for (int e = 0; e < 4; ++e) P[e] = M[e] = 0.0;
-            const __nv_bfloat16* qrow = j.Q + (int64_t)row * j.ldq + (int64_t)head * G * c.d + lane * 4;
-            for (int g = 0; g < G && on; ++g) {
+            const __nv_bfloat16* qrow = j.Q + (int64_t)row * j.ldq + (int64_t)head * G * c.d + (on ? lane * 4 : 0);
+#pragma unroll 4
+            for (int g = 0; g < G; ++g) {
                 const uint2 w = *reinterpret_cast<const uint2*>(qrow + (int64_t)g * c.d);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -497,6 +576,7 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
                     M[e] += x > 0.0 ? 0.0 : x;
                 }
             }
+#pragma unroll 2
             for (int q = mate; q < band; q += tw) {
                 const int page = __shfl_sync(0xffffffffu, page_l, q);
                 double x = 0.0;
@@ -521,13 +601,24 @@ k_cache_select(const CacheView c, const Ragged r, const SelectJob j, int rows, i
                 const unsigned long long k = __shfl_sync(0xffffffffu, own, q);
                 rank += k > own || (k == own && q < lane);       // (the list ascends)
             }
-            if (mate == 0 && lane < band) s[mine] = rank < need ? -SEL_NONE : SEL_NONE;
+            chosen = __ballot_sync(0xffffffffu, lane < band && rank < need);
+            if (!left && mate == 0 && lane < band) s[mine] = rank < need ? -SEL_NONE : SEL_NONE;
             __syncwarp();
-            cut = __uint_as_float(__float_as_uint(above) + (above >= 0.f ? 1u : -1u));   // (the next number above it)
-            if (above == 0.f) cut = 1.4e-45f;
         }
-        if (mate == 0)                                           // (the first warp has what was decided in 64 bits)
+        if (mate != 0) continue;                                 // (the first warp has what was decided in 64 bits)
+        if (left) {
+            const bool ia = va > above || ((ua >> lane & 1u) && (chosen >> (at_a & 31) & 1u));
+            const bool ib = vb > above || ((ub >> lane & 1u) && (chosen >> (at_b & 31) & 1u));
+            const unsigned ma = __ballot_sync(0xffffffffu, ia), mb = __ballot_sync(0xffffffffu, ib);
+            if (ia) idx[first + __popc(ma & before)] = pa;
+            if (ib) idx[first + __popc(ma) + __popc(mb & before)] = pb;
+        } else {
+            float cut = below;                                   // in if s >= cut
+            if (band != need) {                                  // the next number above `above`
+                cut = above == 0.f ? 1.4e-45f : __uint_as_float(__float_as_uint(above) + (above > 0.f ? 1u : -1u));
+            }
             list([&](float x) { return x >= cut; }, [&](int at, int p) { idx[first + at] = p; });
+        }
     }
     if (nb_all <= j.k) return;
     __syncthreads();
@@ -620,11 +711,11 @@ cudaError_t launch_cache_select(ada_ctx* ctx, const CacheView& c, const Ragged& 
     while (rows > 1 && (rows * stride * 4 > 65536 || rows / 2 * (int64_t)r.B >= r.N)) rows >>= 1;
     const int most = 226 * 1024 - (int)sizeof(SelShared);
     if (rows == 1) {
+        const int scores = stride * 4 + SEL_WARPS * SEL_LEFT * 8;
         const cudaError_t e = allow_smem(ctx, 14, k_cache_select<true>, most);
         if (e != cudaSuccess) return e;
-        return launch_k(ctx, k_cache_select<true>, dim3(r.N, c.h_kv), dim3(SEL_THREADS), ((keys > stride * 4 ? keys : stride * 4) + 15) / 16 * 16, s, c, r, j, 1,
-                        stride,
-                        0, ctx->status);
+        return launch_k(ctx, k_cache_select<true>, dim3(r.N, c.h_kv), dim3(SEL_THREADS), ((keys > scores ? keys : scores) + 15) / 16 * 16, s, c, r, j, 1,
+                        stride, 0, ctx->status);
     }
     const int ring = SEL_RING * sel_half(c.d), room = ((keys > ring ? keys : ring) + 15) / 16 * 16;
     const int smem = room + 4 * SEL_ROWS * sel_row(c.d) + rows * stride * 4;
