@@ -491,14 +491,14 @@ def ada_cache_append(ctx: Context, cache: KVCache, K: torch.Tensor, V: torch.Ten
     N, _, ldk = _rows_of(K, "K", cache, None, cache.h_kv)
     _, _, ldv = _rows_of(V, "V", cache, N, cache.h_kv)
     if len_out is None:
-        len_out = torch.empty(B, dtype=torch.int32, device=K.device)
+        len_out = length.new_empty(B)
     else:
         _int32(len_out, "len_out", B, cache.index)
     h = ldq = ldqo = 0
     if Q is not None:
         _, h, ldq = _rows_of(Q, "Q", cache, N)
         if q_out is None:
-            q_out = torch.empty((N, h, cache.d_h), dtype=Q.dtype, device=Q.device)
+            q_out = Q.new_empty((N, h, cache.d_h))
             ldqo = h * cache.d_h
         else:
             _, _, ldqo = _rows_of(q_out, "q_out", cache, N, h)
@@ -538,7 +538,7 @@ def ada_attention_cached(ctx: Context, cache: KVCache, Q: torch.Tensor, off: tor
     B = _ragged(cache, off, length)
     N, h, ldq = _rows_of(Q, "Q", cache)
     if out is None:
-        out = torch.zeros((N, h, cache.d_h), dtype=Q.dtype, device=Q.device)
+        out = Q.new_zeros((N, h, cache.d_h))
     _, _, ldo = _rows_of(out, "out", cache, N, h)
     st = _fast.attention_cached(ctx.addr, cache.addr, B, off, length, N, max_new, Q, h, ldq, cache.dtype, scale, out, ldo,
                                 flags, _stream_of(ctx, stream))
@@ -564,8 +564,8 @@ def ada_select_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: torch.
     B = _ragged(cache, off, length)
     N, h, ldq = _rows_of(Q, "Q", cache)
     if blk_idx is None and blk_cnt is None:
-        blk_idx = torch.empty((N, cache.h_kv, k), dtype=torch.int32, device=Q.device)
-        blk_cnt = torch.empty((N, cache.h_kv), dtype=torch.int32, device=Q.device)
+        blk_idx = length.new_empty((N, cache.h_kv, k))
+        blk_cnt = length.new_empty((N, cache.h_kv))
     elif blk_idx is None or blk_cnt is None:
         raise ValueError("blk_idx and blk_cnt are given together")
     else:
@@ -585,7 +585,7 @@ def ada_attention_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: tor
     N, h, ldq = _rows_of(Q, "Q", cache)
     k = _lists_of(cache, N, blk_idx, blk_cnt)
     if out is None:
-        out = torch.zeros((N, h, cache.d_h), dtype=Q.dtype, device=Q.device)
+        out = Q.new_zeros((N, h, cache.d_h))
     _, _, ldo = _rows_of(out, "out", cache, N, h)
     st = _fast.attention_blocks(ctx.addr, cache.addr, B, off, length, N, Q, h, ldq, cache.dtype, blk_idx, blk_cnt, k, scale,
                                 out, ldo, flags, _stream_of(ctx, stream))

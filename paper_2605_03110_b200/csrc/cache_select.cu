@@ -16,9 +16,10 @@
 // a block scores 16 against the same pages on mma.sync, P and M as two bf16 terms each (products exact, fp32
 // sums); the bounds then come from L2 through a ring of four half stages.
 //
-// Measured (32 heads on 8 key heads of 128): 32 tokens over 512 pages each 21 us, 67 MB = 3.2 TB/s (loads 13 us, the choice 4);
-// 1000 tokens over 257 pages 54 us, bound by issue of the choice's instructions: a warp's row takes 1500.  All
-// scores in 64 bits took 47 and 454 us.
+// Measured (32 heads on 8 key heads of 128): 32 tokens over 512 pages each 17 us, 67 MB = 3.9 TB/s (loads 13 us, the choice 3);
+// 1000 tokens over 257 pages 47 us: a block 3 for the tokens' sums, 9 for the scores, 6 for the choice, 1.7 blocks for
+// every place.  Without leaving pages aside first, every guess at the k-th score counting all of them: 21 and 54 us; all
+// scores in 64 bits: 47 and 454.
 #include "cache_tma.cuh"
 
 namespace ada {

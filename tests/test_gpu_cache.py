@@ -323,6 +323,24 @@ def test_select(ada, ctx, h, hk, d, news, lens):
             assert lists_of(idx, cnt) == want
 
 
+@pytest.mark.parametrize("distinct", [0, 3, 40])
+@pytest.mark.parametrize("news,pages", [([1], 65), ([1], 130), ([1], 512), ([1], 700), ([5], 68), ([5], 257), ([5], 512)])
+def test_select_few_places_of_many_pages(ada, ctx, news, pages, distinct):
+    """Few places, many places, on either side of what a warp keeps for itself; pages all different, or with the bounds of
+    a few, so that scores are equal in groups."""
+    c = Case(ada, 24, 4, 2, 64, 16, news, [16 * pages], drift=0.5)
+    if distinct:
+        for p in range(pages):
+            at, like = int(c.cpu.table[0, p]), int(c.cpu.table[0, (p * 7) % distinct])
+            c.cpu.kmin[at], c.cpu.kmax[at] = c.cpu.kmin[like], c.cpu.kmax[like]
+        c.cache.kmin.copy_(c.cpu.kmin)
+        c.cache.kmax.copy_(c.cpu.kmax)
+    for k, first, last in ((1, 0, 0), (2, 1, 0), (17, 1, 1), (18, 0, 1), (20, 1, 1), (34, 1, 1), (35, 1, 1), (64, 30, 2), (64, 0, 0)):
+        idx, cnt = ada.ada_select_blocks(ctx, c.cache, c.d_Q, c.d_off, c.d_len, k, first, last)
+        fine(ada, ctx)
+        assert lists_of(idx, cnt) == ref.select(c.cpu, c.Q, c.off, c.lens, 2, k, first, last), (k, first, last)
+
+
 def test_select_ties_go_to_the_lower_page(ada, ctx):
     """Pages with the same bounds, and queries of zeros: every score equal."""
     c = Case(ada, 21, 4, 2, 64, 16, [2], [1600])
