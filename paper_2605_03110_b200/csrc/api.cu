@@ -16,7 +16,8 @@ namespace {
 const char* const kKernelNames[K_COUNT] = {
     "norm_gather",     "gram_ffma_tri",    "gram_ffma_cross",
     "gram_tc_tri",     "gram_tc_cross",    "gram_tc_cascade", "split_bf16x3",  "compact_full",
-    "compact_cascade", "nearest_finish",  "step_short",
+    "compact_cascade", "nearest_finish",  "step_short",      "cache_append",    "cache_bounds",
+    "cache_step",      "cache_chunk",     "cache_select",
 };
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }

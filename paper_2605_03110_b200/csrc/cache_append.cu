@@ -366,14 +366,18 @@ cudaError_t launch_cache_append(ada_ctx* ctx, const CacheView& c, const Ragged& 
                                     : (j.pairs ? k_cache_append<16, true, true> : k_cache_append<16, false, true>))
                        : (c.d <= 64 ? (j.pairs ? k_cache_append<8, true, false> : k_cache_append<8, false, false>)
                                     : (j.pairs ? k_cache_append<16, true, false> : k_cache_append<16, false, false>));
+    prof_begin(ctx, K_CACHE_APPEND, s);
     cudaError_t e = launch_k(ctx, kernel, dim3((unsigned)((items + APP_WARPS - 1) / APP_WARPS)), dim3(APP_THREADS), 0, s, c, r, j,
                              shares, ctx->status);
+    prof_end(ctx, s);
     if (e != cudaSuccess) return e;
     if (c.kmin != nullptr && !step) {
         // a sequence of n new tokens writes to at most n and at most (n - 1) / ps + 2 pages
         const int64_t most = (int64_t)(r.N >> c.shift) + 2 * (int64_t)r.B;
         const int pages = (int)(most < r.N ? most : r.N);
+        prof_begin(ctx, K_CACHE_BOUNDS, s);
         e = launch_k(ctx, k_cache_bounds, dim3(pages, c.h_kv), dim3(BND_THREADS), 0, s, c, r, j.rep_cnt);
+        prof_end(ctx, s);
     }
     return e;
 }

@@ -708,8 +708,11 @@ cudaError_t run_chunk(ada_ctx* ctx, const ChunkMaps& maps, const CacheView& c, c
                       cudaStream_t s) {
     cudaError_t e = allow_smem(ctx, 11 + NDB, k_cache_chunk<NDB>, ch_smem<NDB>());                // bits 12, 13
     if (e != cudaSuccess) return e;
-    return launch_k(ctx, k_cache_chunk<NDB>, dim3(ctx->sm_count), dim3(CH_THREADS), ch_smem<NDB>(), s, maps, c, r, j, tq,
-                    ctx->cache_part, ctx->cache_ctr, ctx->status);
+    prof_begin(ctx, K_CACHE_CHUNK, s);
+    e = launch_k(ctx, k_cache_chunk<NDB>, dim3(ctx->sm_count), dim3(CH_THREADS), ch_smem<NDB>(), s, maps, c, r, j, tq,
+                 ctx->cache_part, ctx->cache_ctr, ctx->status);
+    prof_end(ctx, s);
+    return e;
 }
 
 }  // namespace

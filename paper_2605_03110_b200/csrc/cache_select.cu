@@ -711,19 +711,23 @@ cudaError_t launch_cache_select(ada_ctx* ctx, const CacheView& c, const Ragged& 
     int rows = SEL_ROWS;
     while (rows > 1 && (rows * stride * 4 > 65536 || rows / 2 * (int64_t)r.B >= r.N)) rows >>= 1;
     const int most = 226 * 1024 - (int)sizeof(SelShared);
+    cudaError_t e;
     if (rows == 1) {
         const int scores = stride * 4 + SEL_WARPS * SEL_LEFT * 8;
-        const cudaError_t e = allow_smem(ctx, 14, k_cache_select<true>, most);
-        if (e != cudaSuccess) return e;
-        return launch_k(ctx, k_cache_select<true>, dim3(r.N, c.h_kv), dim3(SEL_THREADS), ((keys > scores ? keys : scores) + 15) / 16 * 16, s, c, r, j, 1,
-                        stride, 0, ctx->status);
+        if ((e = allow_smem(ctx, 14, k_cache_select<true>, most)) != cudaSuccess) return e;
+        prof_begin(ctx, K_CACHE_SELECT, s);
+        e = launch_k(ctx, k_cache_select<true>, dim3(r.N, c.h_kv), dim3(SEL_THREADS), ((keys > scores ? keys : scores) + 15) / 16 * 16,
+                     s, c, r, j, 1, stride, 0, ctx->status);
+    } else {
+        const int ring = SEL_RING * sel_half(c.d), room = ((keys > ring ? keys : ring) + 15) / 16 * 16;
+        const int smem = room + 4 * SEL_ROWS * sel_row(c.d) + rows * stride * 4;
+        if ((e = allow_smem(ctx, 15, k_cache_select<false>, most)) != cudaSuccess) return e;
+        prof_begin(ctx, K_CACHE_SELECT, s);
+        e = launch_k(ctx, k_cache_select<false>, dim3(r.N / rows + (r.B < r.N ? r.B : r.N), c.h_kv), dim3(SEL_THREADS), smem, s, c, r,
+                     j, rows, stride, room, ctx->status);
     }
-    const int ring = SEL_RING * sel_half(c.d), room = ((keys > ring ? keys : ring) + 15) / 16 * 16;
-    const int smem = room + 4 * SEL_ROWS * sel_row(c.d) + rows * stride * 4;
-    const cudaError_t e = allow_smem(ctx, 15, k_cache_select<false>, most);
-    if (e != cudaSuccess) return e;
-    return launch_k(ctx, k_cache_select<false>, dim3(r.N / rows + (r.B < r.N ? r.B : r.N), c.h_kv), dim3(SEL_THREADS), smem, s, c, r, j,
-                    rows, stride, room, ctx->status);
+    prof_end(ctx, s);
+    return e;
 }
 
 }  // namespace ada

@@ -616,8 +616,11 @@ cudaError_t run_step(ada_ctx* ctx, const StepMaps& maps, const CacheView& c, con
     auto kernel = k_cache_step<NDB, NT, LIST, TEAM>;
     cudaError_t e = allow_smem(ctx, (NDB - 1) + 2 * (NT - 1) + 4 * (!LIST ? 0 : TEAM == 1 ? 1 : 2), kernel, st_smem<NDB>());   // bits 0 .. 11
     if (e != cudaSuccess) return e;
-    return launch_k(ctx, kernel, dim3(p.grid), dim3(32 * st_warps<NT, TEAM>()), st_smem<NDB>(), s, maps, c, r, j, p.tiles, p.pieces,
-                    ctx->cache_part, ctx->cache_ctr, ctx->status);
+    prof_begin(ctx, K_CACHE_STEP, s);
+    e = launch_k(ctx, kernel, dim3(p.grid), dim3(32 * st_warps<NT, TEAM>()), st_smem<NDB>(), s, maps, c, r, j, p.tiles, p.pieces,
+                 ctx->cache_part, ctx->cache_ctr, ctx->status);
+    prof_end(ctx, s);
+    return e;
 }
 template <bool LIST, int TEAM>
 cudaError_t run_step(ada_ctx* ctx, const StepMaps& maps, const CacheView& c, const Ragged& r, const AttendJob& j,

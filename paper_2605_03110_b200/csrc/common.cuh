@@ -33,6 +33,11 @@ enum KernelId {
     K_COMPACT_CASCADE,
     K_NEAREST_FINISH,
     K_STEP_SHORT,
+    K_CACHE_APPEND,
+    K_CACHE_BOUNDS,
+    K_CACHE_STEP,
+    K_CACHE_CHUNK,
+    K_CACHE_SELECT,
     K_COUNT
 };
 

@@ -671,6 +671,34 @@ def test_another_stream_and_two_contexts_at_once(ada):
         ada.ada_destroy(x)
 
 
+def test_kernel_times_and_launches_without_overlap(ada, ctx):
+    """Every kernel of the calls is in the per-kernel timing; without dependent launches the results are the same."""
+    c = Case(ada, 31, 8, 2, 64, 16, [70, 1], [900, 300])
+    K, V = (torch.randn(71, 2, 64, device="cuda").bfloat16() for _ in range(2))
+
+    def run():
+        pages = ada.KVCache(*(x.clone() for x in (c.cache.K, c.cache.V, c.cache.table, c.cache.kmin, c.cache.kmax)))
+        ada.ada_cache_append(ctx, pages, K, V, c.d_off, i32([830, 299]))
+        out = ada.ada_attention_cached(ctx, pages, c.d_Q, c.d_off, c.d_len, 70)
+        idx, cnt = ada.ada_select_blocks(ctx, pages, c.d_Q, c.d_off, c.d_len, 6)
+        return out, idx, cnt, ada.ada_attention_blocks(ctx, pages, c.d_Q, c.d_off, c.d_len, idx, cnt)
+
+    want = run()
+    ada.ada_profile_enable(ctx, True)
+    ada.ada_set_dependent_launch(ctx, False)
+    try:
+        got = run()
+        times = {k: v for k, v in ada.ada_profile_read(ctx).items() if v[0]}
+    finally:
+        ada.ada_profile_enable(ctx, False)
+        ada.ada_set_dependent_launch(ctx, True)
+    fine(ada, ctx)
+    assert {k: n for k, (n, _) in times.items()} == {"cache_append": 1, "cache_bounds": 1, "cache_step": 2, "cache_chunk": 1,
+                                                     "cache_select": 1}
+    assert all(t > 0 for _, t in times.values())
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
 def test_captured_step(ada, ctx):
     """A decoding step as a graph: append, choose, attend; replayed over growing lengths that live on the device."""
     h, hk, d, ps, k = 8, 2, 64, 16, 4
