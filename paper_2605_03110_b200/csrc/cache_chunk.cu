@@ -5,6 +5,7 @@
 // of TMEM: two score tiles, two accumulators) are a CTA's work item, and both read the same tiles of 128 keys.
 //   warp 0      TMA: queries, and pages of K and V into a ring of slots (one slot = K or V of 128 keys)
 //   warp 1      tcgen05.mma: S_t = Q_t K^T, O_t += P_t V; while tile 0's softmax runs, tile 1's products do
+//   warps 2, 3  look at the values that not every row sees (a chunk's own): a NaN there must not reach the rows before it
 //   warps 4..7  softmax of tile 0, one row per thread: S out of TMEM into registers, 2^(s - m), P back into TMEM as bf16
 //               over its own scores, where the second product takes it from as its left operand
 //   warps 8..11 the same for tile 1 (they have most of the registers: a row's 128 scores stay in them)
@@ -45,6 +46,9 @@ struct ChunkShared {
     int abort_flag[2];
     int start[5];                                 // b, p, head, place within the item: where the CTA's run begins; turn
     long long range[3];                           // first place, one past the last, places per CTA
+    struct { int slot, from, to, found[2]; } look; // values to look at: number of the slot's load (-1: no more), its rows; answers
+    int odd_item;                                 // the CTA's latest item (from 1) with entries in here:
+    int odd[3][128];                              // first key whose value in a column is NaN, inf, -inf (see clean_values)
 };
 template <int NDB> __host__ __device__ constexpr int ch_smem() { return 14 * BLK_BYTES + (int)sizeof(ChunkShared); }
 static_assert(ch_smem<2>() <= 227 * 1024, "shared memory budget");
@@ -195,6 +199,51 @@ __device__ __forceinline__ void exp_pairs(const unsigned (&a)[32], const unsigne
     sum += (u0 + u1) + (v0 + v1);
 }
 
+// Values of keys that some rows of an item see and others do not (a chunk's own tokens, causal), as they lie in a slot, from
+// row `from` to row `to`: one that is not finite would meet the zero probabilities of the rows before it.  So it becomes
+// zero for all of them, and odd[][column] says from which key on a row has seen one: such rows get it back at the item's
+// end (restore_values).  Rows in shared memory are 128 bytes of 64 elements, 16-byte pieces swizzled.
+// Who looks at them: the issuing warp itself made a mixed batch of 8 sequences 142 -> 155 us and 2048 tokens after 6145
+// 263 -> 267; two warps that are otherwise idle, a key tile ahead of it, 146 and 264.
+template <int NDB>
+__device__ __forceinline__ void clean_values(unsigned char* v, int from, int to, int key0, int lane, ChunkShared& sh) {
+    for (int q = from * 8 + lane; q < to * 8; q += 32)
+        for (int db = 0; db < NDB; ++db) {
+            uint4* at = reinterpret_cast<uint4*>(v + db * BLK_BYTES + q * 16);
+            uint4 x = *at;
+            if (!nonfinite8(x)) continue;
+            unsigned* u = reinterpret_cast<unsigned*>(&x);
+            for (int e = 0; e < 8; ++e) {
+                const unsigned h = u[e >> 1] >> (16 * (e & 1)) & 0xffffu;
+                if ((h & 0x7f80u) != 0x7f80u) continue;
+                const int kind = (h & 0x7fu) != 0u ? 0 : h >> 15 ? 2 : 1;
+                atomicMin(&sh.odd[kind][db * 64 + (((q & 7) ^ ((q >> 3) & 7)) << 3) + e], key0 + (q >> 3));
+                u[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
+            }
+            *at = x;
+        }
+}
+// the accumulator in TMEM of a row that sees `lim` keys
+template <int NDB>
+__device__ __forceinline__ void restore_values(unsigned t_o, int lim, const ChunkShared& sh) {
+#pragma unroll 1
+    for (int q = 0; q < NDB * 2; ++q) {
+        unsigned y[32];
+        tmem_ld32_issue(t_o + q * 32, y);
+        tmem_ld_wait(y);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const int col = q * 32 + e;
+            float x = __uint_as_float(y[e]);
+            if (lim > sh.odd[0][col]) x = NAN;
+            if (lim > sh.odd[1][col]) x += INFINITY;
+            if (lim > sh.odd[2][col]) x -= INFINITY;
+            y[e] = __float_as_uint(x);
+        }
+        tmem_st32(t_o + q * 32, y);
+    }
+}
+
 template <int NDB>
 __global__ void __launch_bounds__(CH_THREADS, 1)
 k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const Ragged r, const AttendJob j, int tq,
@@ -222,6 +271,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
         }
         sh.abort_flag[0] = 0;
         sh.abort_flag[1] = wait_limit_units(false);
+        sh.odd_item = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -384,9 +434,30 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
         const unsigned lead = elect_one();
         const unsigned idesc_s = instr_desc(CH_KEYS);
         const unsigned idesc_o = instr_desc(NDB * 64) | (1u << 16);          // right operand MN-major
+        // asks warps 2 and 3 for the values of unit u, load number `slot`, a unit ahead, if not every row sees them all; one
+        // request at a time: it has been answered before the next one is made
+        bool asked = false;
+        auto look = [&](int u, unsigned slot) {
+            const int key0 = (it.ku + u) * CH_KEYS;
+            if (it.first_lim - key0 >= CH_KEYS) return;
+            if (lane == 0) {
+                sh.look.slot = (int)slot;
+                sh.look.from = max(it.first_lim - key0, 0);
+                sh.look.to = min(max(it.kv - key0, 0), CH_KEYS);
+            }
+            __syncwarp();
+            asm volatile("bar.arrive 1, 96;" ::: "memory");
+            asked = true;
+        };
+        auto looked = [&]() {
+            asm volatile("bar.sync 2, 96;" ::: "memory");
+            asked = false;
+            return (sh.look.found[0] | sh.look.found[1]) != 0;
+        };
         for (int k = 0; ok && work.next(it, r, c, tq, j.causal, j.max_new, j.few); ++k) {
             const int nt[2] = {ChunkWork::tiles_of(it, 0), ChunkWork::tiles_of(it, 1)};
             const int two = it.units[1] > 0 ? 2 : 1;
+            look(0, got + 1);
             ok = mbar_wait(&sh.q_full, (unsigned)k & 1u, abort_flag, 35);
             auto wait_slot = [&](unsigned i, int where) {
                 ok = ok && mbar_wait(&sh.full[i % SLOTS], (i / SLOTS) & 1u, abort_flag, where);
@@ -413,20 +484,28 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 const unsigned sv = got + 1, sk = got + 2;
                 wait_slot(sv, 38);
                 if (!ok) break;
-                // values of slots behind the sequence's length meet probabilities of zero: they must not be NaN
-                const int live = it.kv - (it.ku + u) * CH_KEYS;
-                if (live < CH_KEYS) {
-                    unsigned char* v = ring + (sv % SLOTS) * SLOT_BYTES;
-                    for (int q = max(live, 0) * 8 + lane; q < CH_KEYS * 8; q += 32)
-#pragma unroll
-                        for (int db = 0; db < NDB; ++db)
-                            *reinterpret_cast<uint4*>(v + db * BLK_BYTES + q * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                }
                 const bool ahead = u + 1 < it.take;
                 if (ahead) wait_slot(sk, 37);
                 if (!ok) break;
+                // values that a row does not see meet probabilities of zero: warps 2 and 3 have looked at them
+                if (asked) {
+                    if (looked()) {
+                        if (sh.odd_item != k + 1) {                          // the entries of items before: nobody needs them any more
+                            for (int t = 0; t < 2; ++t)
+                                if (n_o[t] > 0) ok = ok && mbar_wait(&sh.o_empty[t], (n_o[t] - 1u) & 1u, abort_flag, 44);
+                            ok = __all_sync(0xffffffffu, ok);
+                            if (!ok) break;
+                            for (int q = lane; q < 3 * 128; q += 32) sh.odd[0][q] = INT_MAX;
+                            __syncwarp();
+                        }
+                        clean_values<NDB>(ring + (sv % SLOTS) * SLOT_BYTES, sh.look.from, sh.look.to, (it.ku + u) * CH_KEYS, lane, sh);
+                        if (lane == 0) sh.odd_item = k + 1;
+                        __threadfence_block();
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                }
+                if (ahead) look(u + 1, sv + 2);
                 for (int t = 0; t < two; ++t) {
                     if (u >= nt[t]) continue;
                     // the accumulator is overwritten: the previous item's rows have been read out
@@ -458,7 +537,40 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 }
             }
         }
-    } else if (warp >= 4) {
+        if (asked) looked();
+        if (lane == 0) sh.look.slot = -1;
+        __syncwarp();
+        asm volatile("bar.arrive 1, 96;" ::: "memory");
+    } else if (warp < 4) {
+        // ------------------------------------------------ values that meet zero probabilities (see clean_values)
+        bool ok = true;
+        for (;;) {
+            asm volatile("bar.sync 1, 96;" ::: "memory");
+            const int slot = sh.look.slot, from = sh.look.from, to = sh.look.to;
+            if (slot < 0) break;
+            // (the slot's load before this one is long done: warp 1 has waited for it)
+            if (ok) ok = mbar_wait(&sh.full[(unsigned)slot % SLOTS], ((unsigned)slot / SLOTS) & 1u, abort_flag, 45);
+            ok = __all_sync(0xffffffffu, ok);
+            bool odd = false;
+            if (ok) {
+                unsigned char* v = ring + ((unsigned)slot % SLOTS) * SLOT_BYTES;
+                const int i = (warp - 2) * 32 + lane;
+#pragma unroll 4
+                for (int q = from * 8 + i; q < to * 8; q += 64)
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db) odd |= nonfinite8(*reinterpret_cast<const uint4*>(v + db * BLK_BYTES + q * 16));
+                for (int q = to * 8 + i; q < CH_KEYS * 8; q += 64)           // nobody's: whatever it is becomes zero
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db)
+                        *reinterpret_cast<uint4*>(v + db * BLK_BYTES + q * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            odd = __any_sync(0xffffffffu, odd);
+            if (lane == 0) sh.look.found[warp - 2] = odd;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            asm volatile("bar.arrive 2, 96;" ::: "memory");
+        }
+    } else {
         // ------------------------------------------------ softmax and output
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int quad = warp & 3, t = (warp - 4) >> 2;
@@ -468,7 +580,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
         const int tok = i / G, g = i - tok * G;                             // within the tile
         bool ok = true;
         unsigned n_s = 0, n_o = 0;
-        while (work.next(it, r, c, tq, j.causal, j.max_new, j.few)) {
+        for (int k = 1; work.next(it, r, c, tq, j.causal, j.max_new, j.few); ++k) {
             if (it.units[t] == 0 && t == 1) continue;                       // no rows in this tile
             const int nt = ChunkWork::tiles_of(it, t);
             const int tok_i = t * tq + tok;                                 // within the item
@@ -551,6 +663,8 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 ++n_o;
                 tcgen05_fence_after();
+                // (no later item's number can be there before this one's o_empty)
+                if (sh.odd_item == k) restore_values<NDB>(t_o, lim, sh);
             }
             __nv_bfloat16* dst = j.out + (int64_t)(it.row0 + tok_i) * j.ldo + ((int64_t)it.head * G + g) * c.d;
             if (it.pieces == 1) {

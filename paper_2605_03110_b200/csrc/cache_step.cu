@@ -478,27 +478,74 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
             wait_slot(51);
             if (ok) {
                 const int st = used % SLOTS;
-                // values of slots that hold nothing of this sequence must not meet a zero probability as NaN
-                if (base.x + 15 >= s.len || base.y + 15 >= s.len) {
+                // Values that a row does not see must not meet its zero probability as a NaN or an infinity: those of slots that
+                // hold nothing of this sequence become zeros; if one of a later token is not finite, every token gets its products
+                // with zeros from its own limit on.
+                bool apart = false;
+                if (base.x + 15 >= lim_all || base.y + 15 >= lim_all) {
                     unsigned char* v = ring + st * st_slot_bytes<NDB>();
+                    bool odd = false;
                     for (int q = lane; q < GK * NDB * 8; q += 32) {
                         const int key = (q >> 3) & 31, db = q >> 8;
-                        if ((key < 16 ? base.x + key : base.y + key - 16) >= s.len)
-                            *reinterpret_cast<uint4*>(v + db * BLOCK + key * 128 + (q & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        const int pos = key < 16 ? base.x + key : base.y + key - 16;
+                        uint4* at = reinterpret_cast<uint4*>(v + db * BLOCK + key * 128 + (q & 7) * 16);
+                        if (pos >= s.len) *at = make_uint4(0u, 0u, 0u, 0u);
+                        else if (!LIST && pos >= lim_all) odd = odd || nonfinite8(*at);
                     }
+                    if (!LIST) apart = __any_sync(0xffffffffu, odd);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the slot's next load comes through the async proxy)
                     __syncwarp();
                 }
                 const unsigned vt = ring_u + st * st_slot_bytes<NDB>();
+                auto v_at = [&](int mt, int d) {
+                    return vt + (d >> 2) * BLOCK + (mt * 16 + v_key) * 128 + ((((d & 3) * 2 + v_ch) ^ (v_key & 7)) << 4);
+                };
+                if (!apart) {
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
+                    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                    for (int d = 0; d < KS; ++d) {
-                        unsigned a[4];
-                        ldsm4t(vt + (d >> 2) * BLOCK + (mt * 16 + v_key) * 128 + ((((d & 3) * 2 + v_ch) ^ (v_key & 7)) << 4), a);
+                        for (int d = 0; d < KS; ++d) {
+                            unsigned a[4];
+                            ldsm4t(v_at(mt, d), a);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16816(o[d][nt], a, pf[mt][nt][0], pf[mt][nt][1]);
+                            for (int nt = 0; nt < NT; ++nt) mma16816(o[d][nt], a, pf[mt][nt][0], pf[mt][nt][1]);
+                        }
+                } else {
+                    // from the last token, which sees the most, to the first; of each product the token's own rows are kept
+#pragma unroll 1
+                    for (int t = (s.rows + G - 1) / G - 1; t >= 0; --t) {
+                        unsigned char* v = ring + st * st_slot_bytes<NDB>();
+                        for (int q = lane; q < GK * NDB * 8; q += 32) {
+                            const int key = (q >> 3) & 31, db = q >> 8;
+                            if ((key < 16 ? base.x + key : base.y + key - 16) >= lim_all + t)
+                                *reinterpret_cast<uint4*>(v + db * BLOCK + key * 128 + (q & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int d = 0; d < KS; ++d) {
+                            float x[NT][4];
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) x[nt][e] = o[d][nt][e];
+#pragma unroll
+                            for (int mt = 0; mt < 2; ++mt) {
+                                unsigned a[4];
+                                ldsm4t(v_at(mt, d), a);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) mma16816(x[nt], a, pf[mt][nt][0], pf[mt][nt][1]);
+                            }
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if ((nt * 8 + c0 + (e & 1)) / G == t) o[d][nt][e] = x[nt][e];
+                        }
+                        __syncwarp();                 // all lanes have read the values
                     }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
             }
             release();
         }

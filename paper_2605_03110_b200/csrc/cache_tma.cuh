@@ -84,6 +84,17 @@ static __device__ __forceinline__ void mma16816(float (&c)[4], const unsigned (&
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// one of eight bf16 is NaN or infinite (an exponent of all ones: 0 times it is NaN)
+static __device__ __forceinline__ bool nonfinite8(const uint4& w) {
+    const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
+    __nv_bfloat162 x = zero;
+    const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&u[i]), zero, x);
+    const unsigned y = *reinterpret_cast<const unsigned*>(&x);
+    return (y & 0x7fff7fffu) != 0u;
+}
+
 // transposes an 8 x 8 matrix of 16-bit elements held as a matrix fragment (two elements of a row per lane)
 static __device__ __forceinline__ unsigned transposed(unsigned x) {
     unsigned y;

@@ -259,6 +259,73 @@ def test_nan_and_infinity_that_a_token_sees(ada, ctx, n, lists):
             assert bool(out.cpu().isfinite().all(-1)[~bad].all())
 
 
+def attend_by(ada, ctx, c, how):
+    """A call of either kind over all that the new tokens see: dense, causal or not, or over lists of every page."""
+    if how != "lists":
+        return ada.ada_attention_cached(ctx, c.cache, c.d_Q, c.d_off, c.d_len, c.max_new, flags=int(how == "causal"))
+    pages = c.cache.table.shape[1] - 2
+    idx = torch.arange(pages, dtype=torch.int32, device="cuda").expand(c.N, c.hk, pages).contiguous()
+    cnt = torch.zeros((c.N, c.hk), dtype=torch.int32)
+    for b, n in enumerate(c.lens):
+        cnt[c.off[b]:c.off[b + 1]] = -(-n // c.ps)
+    return ada.ada_attention_blocks(ctx, c.cache, c.d_Q, c.d_off, c.d_len, idx, cnt.cuda())
+
+
+@pytest.mark.parametrize("how", ["causal", "all", "lists"])
+@pytest.mark.parametrize("h,hk,d,ps,n,length", [(4, 2, 128, 32, 1, 900), (4, 2, 128, 32, 3, 900), (2, 2, 128, 64, 16, 500),
+                                                (3, 1, 48, 16, 4, 129), (4, 2, 128, 32, 90, 900), (4, 2, 128, 32, 700, 900),
+                                                (16, 1, 64, 128, 130, 130), (6, 1, 80, 16, 60, 40)])
+def test_nan_and_infinity_in_values(ada, ctx, h, hk, d, ps, n, length, how):
+    """A value that is NaN or infinite makes its element so in the rows that see its slot, and changes nothing else: not a
+    bit of the rows before it, whose probability of that slot is zero."""
+    c = Case(ada, 25, h, hk, d, ps, [n], [length])
+    clean = attend_by(ada, ctx, c, how).cpu()
+    fine(ada, ctx)
+    j, heads = hk - 1, slice((hk - 1) * (h // hk), h)
+    limit = torch.tensor([ref.sees(n, length, i, how != "all") for i in range(n)])
+    first = max(length - n, 0)
+    for slot in sorted({0, 5, 127, first, first + 1, first + n // 2, length - 60, length - 2, length - 1}):
+        if not 0 < slot + 1 <= length:
+            continue
+        sees = limit > slot
+        for values, elements in (((math.nan,), [7]), ((math.inf,), [0]), ((-math.inf,), [d - 1]), ((math.nan,), list(range(d))),
+                                 ((math.inf, -math.inf), [d // 2 + 3]), ((-math.inf, math.nan), [1, d - 2])):
+            want = clean.float()
+            c.cache.V.copy_(c.cpu.V)
+            for k, value in enumerate(values):               # the second one in the slot before
+                at = max(slot - k, 0)
+                c.cache.V[int(c.cpu.table[0, at // ps]), j, at % ps, elements] = value
+                for e in elements:
+                    before = want[:, heads, e]
+                    new = torch.where((limit > at).view(-1, 1), torch.full_like(before, value), before)
+                    if k > 0 and at < slot:                  # both: +inf - inf and NaN are NaN
+                        new = torch.where(sees.view(-1, 1), torch.full_like(before, math.nan), new)
+                    want[:, heads, e] = new
+            got = attend_by(ada, ctx, c, how).cpu().float()
+            fine(ada, ctx)
+            assert torch.equal(got.isnan(), want.isnan()), (slot, values, elements)
+            assert torch.equal(got.nan_to_num(9e9, 8e9, -8e9), want.nan_to_num(9e9, 8e9, -8e9)), (slot, values, elements)
+
+
+@pytest.mark.parametrize("news,lens,h,hk", [([40] * 20, [40 + 31 * b for b in range(20)], 16, 16),
+                                            ([60, 3, 1, 200, 17], [700, 90, 4, 200, 17], 8, 2),
+                                            ([300, 300], [2500, 280], 4, 1)])
+def test_nan_in_values_of_one_sequence(ada, ctx, news, lens, h, hk):
+    """Many items of many sequences and heads on an SM: a NaN in the last value of some of them is seen by that token alone."""
+    c = Case(ada, 26, h, hk, 64, 32, news, lens)
+    clean = attend_by(ada, ctx, c, "causal").cpu()
+    fine(ada, ctx)
+    for b, j in {(0, 0), (len(news) // 2, hk - 1), (len(news) - 1, hk // 2), (1, 0)}:
+        c.cache.V.copy_(c.cpu.V)
+        at = lens[b] - 1
+        c.cache.V[int(c.cpu.table[b, at // 32]), j, at % 32, 20] = math.nan
+        got = attend_by(ada, ctx, c, "causal").cpu()
+        fine(ada, ctx)
+        want = clean.clone()
+        want[c.off[b + 1] - 1, j * (h // hk):(j + 1) * (h // hk), 20] = math.nan
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num()), (b, j)
+
+
 @pytest.mark.parametrize("news,lens", [([1] * 5, [3, 900, 64, 2000, 1]), ([200], [5000]), ([1, 90, 2, 300], [700, 90, 2, 1000])])
 def test_output_over_the_queries(ada, ctx, news, lens):
     c = Case(ada, 22, 8, 2, 128, 64, news, lens)
