@@ -8,6 +8,7 @@ built (python -m paper_2605_03110_b200.build) loading fails loudly.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -160,6 +161,23 @@ def _stream_of(ctx, stream) -> int:
     return stream.cuda_stream
 
 
+_NO_SWITCH = contextlib.nullcontext()
+
+
+def _on(stream, like: torch.Tensor):
+    """Where a call makes its own outputs: on the stream that its kernels run on.  Filled on another one, they could be
+    cleared after the kernel has written them, and their memory could still be in use there."""
+    return _NO_SWITCH if stream is None or like.get_device() < 0 else torch.cuda.stream(stream)
+
+
+def _fresh(stream, make, like: torch.Tensor, shape):
+    """_on for one tensor make(shape), with less to do where no stream was passed."""
+    if stream is None:
+        return make(shape)
+    with _on(stream, like):
+        return make(shape)
+
+
 def _raise(st: int, where: str) -> None:
     raise AdaError(st, where)
 
@@ -256,9 +274,10 @@ def ada_normalize(ctx: Context, X: torch.Tensor, want_xhat=False, rep_idx=None, 
                   stream=None):
     """Returns (inv_norm, Xhat or None, Xrep or None)."""
     X, B, T, d, ldx = _shape(X)
-    inv = torch.empty((B, T), dtype=torch.float32, device=X.device)
-    xhat = torch.empty((B, T, d), dtype=X.dtype, device=X.device) if want_xhat else None
-    xrep = torch.zeros((B, T, d), dtype=X.dtype, device=X.device) if rep_idx is not None else None
+    with _on(stream, X):
+        inv = torch.empty((B, T), dtype=torch.float32, device=X.device)
+        xhat = torch.empty((B, T, d), dtype=X.dtype, device=X.device) if want_xhat else None
+        xrep = torch.zeros((B, T, d), dtype=X.dtype, device=X.device) if rep_idx is not None else None
     _check(lib().ada_normalize(ctx.h, X.data_ptr(), B, T, d, ldx, dtype_of(X), _ptr(xhat),
                                inv.data_ptr(), _ptr(rep_idx), _ptr(rep_cnt), _ptr(xrep),
                                _stream(stream)), "ada_normalize")
@@ -270,12 +289,13 @@ def ada_select_full(ctx: Context, X: torch.Tensor, tau: float, rep_idx=None, rep
     """Definition 1.  Returns (rep_idx[B,T] int32, rep_cnt[B] int32, gamma[B,T] or None)."""
     X, B, T, d, ldx = _shape(X)
     dev = X.device
-    if rep_idx is None:
-        rep_idx = torch.empty((B, T), dtype=torch.int32, device=dev)
-    if rep_cnt is None:
-        rep_cnt = torch.empty((B,), dtype=torch.int32, device=dev)
-    if gamma is None and want_gamma:
-        gamma = torch.empty((B, T), dtype=torch.float32, device=dev)
+    with _on(stream, X):
+        if rep_idx is None:
+            rep_idx = torch.empty((B, T), dtype=torch.int32, device=dev)
+        if rep_cnt is None:
+            rep_cnt = torch.empty((B,), dtype=torch.int32, device=dev)
+        if gamma is None and want_gamma:
+            gamma = torch.empty((B, T), dtype=torch.float32, device=dev)
     st = _fast.select_full(ctx.addr, X, B, T, d, ldx, dtype_of(X), tau, rep_idx, rep_cnt, gamma, _stream(stream))
     if st:
         _raise(st, "ada_select_full")
@@ -304,7 +324,8 @@ def ada_cascade_step(ctx: Context, X: torch.Tensor, tau: float, rep_in: torch.Te
     """Algorithm 1.  `out` buffers are reused when given."""
     X, B, T, d, ldx = _shape(X)
     if out is None:
-        out = CascadeOut(B, T, X.device, want_gamma)
+        with _on(stream, X):
+            out = CascadeOut(B, T, X.device, want_gamma)
     st = _fast.cascade_step(ctx.addr, X, B, T, d, ldx, dtype_of(X), tau, rep_in, rep_in_cnt, out.rep_out,
                             out.rep_out_cnt, out.add_idx, out.add_cnt, out.rem_idx, out.rem_cnt, out.gamma_rep,
                             out.gamma_cross, flags, _stream(stream))
@@ -325,7 +346,8 @@ def ada_cascade_step_adaptive(ctx: Context, X: torch.Tensor, tau_state: torch.Te
     if policy is not None and not isinstance(policy, TauPolicy):
         raise C.ArgumentError("policy must be a TauPolicy")
     if out is None:
-        out = CascadeOut(B, T, X.device, want_gamma)
+        with _on(stream, X):
+            out = CascadeOut(B, T, X.device, want_gamma)
     st = _fast.cascade_step_adaptive(
         ctx.addr, X, B, T, d, ldx, dtype_of(X), tau_state, None if policy is None else C.addressof(policy), rep_in,
         rep_in_cnt, out.rep_out, out.rep_out_cnt, out.add_idx, out.add_cnt, out.rem_idx, out.rem_cnt, out.gamma_rep,
@@ -350,12 +372,13 @@ def ada_select_full_heads(ctx: Context, X: torch.Tensor, tau: float, rep_idx=Non
     gamma[h,T] or None)."""
     T, h, d_h, ldx = _shape_heads(X)
     dev = X.device
-    if rep_idx is None:
-        rep_idx = torch.empty((h, T), dtype=torch.int32, device=dev)
-    if rep_cnt is None:
-        rep_cnt = torch.empty((h,), dtype=torch.int32, device=dev)
-    if gamma is None and want_gamma:
-        gamma = torch.empty((h, T), dtype=torch.float32, device=dev)
+    with _on(stream, X):
+        if rep_idx is None:
+            rep_idx = torch.empty((h, T), dtype=torch.int32, device=dev)
+        if rep_cnt is None:
+            rep_cnt = torch.empty((h,), dtype=torch.int32, device=dev)
+        if gamma is None and want_gamma:
+            gamma = torch.empty((h, T), dtype=torch.float32, device=dev)
     st = _fast.select_full_heads(ctx.addr, X, T, h, d_h, ldx, dtype_of(X), tau, rep_idx, rep_cnt, gamma,
                                  _stream(stream))
     if st:
@@ -369,7 +392,8 @@ def ada_cascade_step_heads(ctx: Context, X: torch.Tensor, tau: float, rep_in: to
     """Section 8.5: Algorithm 1 per head of X (T, h, d_h); lists are [h, T], counts [h]."""
     T, h, d_h, ldx = _shape_heads(X)
     if out is None:
-        out = CascadeOut(h, T, X.device, want_gamma)
+        with _on(stream, X):
+            out = CascadeOut(h, T, X.device, want_gamma)
     st = _fast.cascade_step_heads(ctx.addr, X, T, h, d_h, ldx, dtype_of(X), tau, rep_in, rep_in_cnt, out.rep_out,
                                   out.rep_out_cnt, out.add_idx, out.add_cnt, out.rem_idx, out.rem_cnt, out.gamma_rep,
                                   out.gamma_cross, flags, _stream(stream))
@@ -382,8 +406,9 @@ def ada_nearest_rep(ctx: Context, X: torch.Tensor, rep_idx: torch.Tensor, rep_cn
                     want_gamma=True, stream=None):
     """Section 2.3.  Returns (nearest_idx[B,T] int32, nearest_gamma[B,T] or None)."""
     X, B, T, d, ldx = _shape(X)
-    near = torch.empty((B, T), dtype=torch.int32, device=X.device)
-    g = torch.empty((B, T), dtype=torch.float32, device=X.device) if want_gamma else None
+    with _on(stream, X):
+        near = torch.empty((B, T), dtype=torch.int32, device=X.device)
+        g = torch.empty((B, T), dtype=torch.float32, device=X.device) if want_gamma else None
     st = _fast.nearest_rep(ctx.addr, X, B, T, d, ldx, dtype_of(X), rep_idx, rep_cnt, near, g, _stream(stream))
     if st:
         _raise(st, "ada_nearest_rep")
@@ -401,7 +426,8 @@ def ada_attention_reps(ctx: Context, Q: torch.Tensor, K: torch.Tensor, V: torch.
     if K.shape != shape or V.shape != shape or K.stride() != strides or V.stride() != strides:
         raise ValueError("Q, K, V must share shape and strides")
     if out is None:
-        out = torch.zeros((T, h, d_h), dtype=torch.float32, device=Q.device)
+        with _on(stream, Q):
+            out = torch.zeros((T, h, d_h), dtype=torch.float32, device=Q.device)
     st = _fast.attention_reps(ctx.addr, Q, K, V, T, h, d_h, ld, dtype_of(Q), rep_idx, rep_cnt, nearest_idx, out,
                               out.stride(0), flags, _stream(stream))
     if st:
@@ -491,14 +517,14 @@ def ada_cache_append(ctx: Context, cache: KVCache, K: torch.Tensor, V: torch.Ten
     N, _, ldk = _rows_of(K, "K", cache, None, cache.h_kv)
     _, _, ldv = _rows_of(V, "V", cache, N, cache.h_kv)
     if len_out is None:
-        len_out = length.new_empty(B)
+        len_out = _fresh(stream, length.new_empty, length, B)
     else:
         _int32(len_out, "len_out", B, cache.index)
     h = ldq = ldqo = 0
     if Q is not None:
         _, h, ldq = _rows_of(Q, "Q", cache, N)
         if q_out is None:
-            q_out = Q.new_empty((N, h, cache.d_h))
+            q_out = _fresh(stream, Q.new_empty, Q, (N, h, cache.d_h))
             ldqo = h * cache.d_h
         else:
             _, _, ldqo = _rows_of(q_out, "q_out", cache, N, h)
@@ -538,7 +564,7 @@ def ada_attention_cached(ctx: Context, cache: KVCache, Q: torch.Tensor, off: tor
     B = _ragged(cache, off, length)
     N, h, ldq = _rows_of(Q, "Q", cache)
     if out is None:
-        out = Q.new_zeros((N, h, cache.d_h))
+        out = _fresh(stream, Q.new_zeros, Q, (N, h, cache.d_h))
     _, _, ldo = _rows_of(out, "out", cache, N, h)
     st = _fast.attention_cached(ctx.addr, cache.addr, B, off, length, N, max_new, Q, h, ldq, cache.dtype, scale, out, ldo,
                                 flags, _stream_of(ctx, stream))
@@ -564,8 +590,8 @@ def ada_select_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: torch.
     B = _ragged(cache, off, length)
     N, h, ldq = _rows_of(Q, "Q", cache)
     if blk_idx is None and blk_cnt is None:
-        blk_idx = length.new_empty((N, cache.h_kv, k))
-        blk_cnt = length.new_empty((N, cache.h_kv))
+        blk_idx = _fresh(stream, length.new_empty, length, (N, cache.h_kv, k))
+        blk_cnt = _fresh(stream, length.new_empty, length, (N, cache.h_kv))
     elif blk_idx is None or blk_cnt is None:
         raise ValueError("blk_idx and blk_cnt are given together")
     else:
@@ -585,7 +611,7 @@ def ada_attention_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: tor
     N, h, ldq = _rows_of(Q, "Q", cache)
     k = _lists_of(cache, N, blk_idx, blk_cnt)
     if out is None:
-        out = Q.new_zeros((N, h, cache.d_h))
+        out = _fresh(stream, Q.new_zeros, Q, (N, h, cache.d_h))
     _, _, ldo = _rows_of(out, "out", cache, N, h)
     st = _fast.attention_blocks(ctx.addr, cache.addr, B, off, length, N, Q, h, ldq, cache.dtype, blk_idx, blk_cnt, k, scale,
                                 out, ldo, flags, _stream_of(ctx, stream))

@@ -209,6 +209,69 @@ def test_call_tensors(ada):
             call()
 
 
+def test_outputs_are_made_on_the_stream_of_the_call(ada, monkeypatch):
+    """What a call allocates or clears for itself is ordered with its kernels: made under the stream that was passed."""
+    import contextlib
+    from types import SimpleNamespace
+    at, made = [None], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        at.append(stream)
+        yield
+        at.pop()
+
+    class OnGPU(torch.Tensor):
+        """A CPU tensor that says it is on a GPU."""
+        def get_device(self):
+            return 0
+
+        def new_empty(self, *a, **k):
+            made.append(at[-1])
+            return super().new_empty(*a, **k)
+
+        def new_zeros(self, *a, **k):
+            made.append(at[-1])
+            return super().new_zeros(*a, **k)
+
+    def count(make):
+        def counted(*a, **k):
+            made.append(at[-1])
+            return make(*a, **k).as_subclass(OnGPU)
+        return counted
+
+    g = lambda t: t.as_subclass(OnGPU)                                                       # noqa: E731
+    stream, ctx = SimpleNamespace(cuda_stream=0), SimpleNamespace(addr=None, h=None, device=0)
+    c = ada.KVCache(g(bf(5, 2, 16, 64)), g(bf(5, 2, 16, 64)), g(torch.zeros((3, 4), dtype=torch.int32)), g(bf(5, 2, 64)),
+                    g(bf(5, 2, 64)))
+    Q, K, off, n = g(bf(7, 4, 64)), g(bf(7, 2, 64)), g(i32(0, 3, 7)), g(i32(5, 9))
+    idx, cnt = g(torch.zeros((7, 2, 4), dtype=torch.int32)), g(torch.zeros((7, 2), dtype=torch.int32))
+    X, lists, one = g(bf(1, 7, 256)), g(torch.zeros((1, 7), dtype=torch.int32)), g(i32(1))
+    heads = g(torch.zeros((4, 7), dtype=torch.int32))
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch, "empty", count(torch.empty))
+    monkeypatch.setattr(torch, "zeros", count(torch.zeros))
+    for outputs, call in (
+            (1, lambda: ada.ada_attention_cached(ctx, c, Q, off, n, 4, stream=stream)),
+            (0, lambda: ada.ada_attention_cached(ctx, c, Q, off, n, 4, out=Q, stream=stream)),
+            (1, lambda: ada.ada_attention_blocks(ctx, c, Q, off, n, idx, cnt, stream=stream)),
+            (2, lambda: ada.ada_select_blocks(ctx, c, Q, off, n, 4, stream=stream)),
+            (0, lambda: ada.ada_select_blocks(ctx, c, Q, off, n, 4, blk_idx=idx, blk_cnt=cnt, stream=stream)),
+            (2, lambda: ada.ada_cache_append(ctx, c, K, K, off, n, Q=Q, stream=stream)),
+            (1, lambda: ada.ada_cache_append(ctx, c, K, K, off, n, stream=stream)),
+            (1, lambda: ada.ada_attention_reps(ctx, Q, Q, Q, lists[0], one, stream=stream)),
+            (3, lambda: ada.ada_normalize(ctx, X, want_xhat=True, rep_idx=lists, rep_cnt=one, stream=stream)),
+            (3, lambda: ada.ada_select_full(ctx, X, 0.3, stream=stream)),
+            (8, lambda: ada.ada_cascade_step(ctx, X, 0.3, lists, one, stream=stream)),
+            (2, lambda: ada.ada_nearest_rep(ctx, X, lists, one, stream=stream)),
+            (3, lambda: ada.ada_select_full_heads(ctx, Q, 0.3, stream=stream)),
+            (8, lambda: ada.ada_cascade_step_heads(ctx, Q, 0.3, heads, heads[:, 0], stream=stream))):
+        made.clear()
+        with pytest.raises(ada.AdaError) as e:             # (there is no context)
+            call()
+        assert e.value.status == 1 and made == [stream] * outputs
+
+
 def test_reference_against_dense_attention():
     """The loops of the reference against torch's attention in 64 bits, and its rotation against complex numbers."""
     g = torch.Generator().manual_seed(0)

@@ -738,6 +738,31 @@ def test_another_stream_and_two_contexts_at_once(ada):
         ada.ada_destroy(x)
 
 
+def test_fresh_outputs_on_another_stream(ada):
+    """A call on another stream than the current one, which has a long queue: its outputs are its own, cleared in time."""
+    own = ada.ada_create(1, 128, 128, ada.ADA_BF16)
+    cases = [Case(ada, 72 + i, 8, 2, 128, 64, n, l) for i, (n, l) in enumerate([([1, 1], [5000, 900]), ([300], [3000])])]
+
+    def run(c, **kw):
+        out = ada.ada_attention_cached(own, c.cache, c.d_Q, c.d_off, c.d_len, c.max_new, **kw)
+        idx, cnt = ada.ada_select_blocks(own, c.cache, c.d_Q, c.d_off, c.d_len, 5, **kw)
+        return out, idx, cnt, ada.ada_attention_blocks(own, c.cache, c.d_Q, c.d_off, c.d_len, idx, cnt, **kw)
+
+    want = [run(c) for c in cases]
+    X = torch.randn((8192, 8192), device="cuda").bfloat16()
+    Y = torch.empty_like(X)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        for _ in range(20):
+            torch.matmul(X, X, out=Y)
+        got = [run(c, stream=side) for c in cases]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for a, b in zip(got, want) for x, y in zip(a, b))
+    fine(ada, own)
+    ada.ada_destroy(own)
+
+
 def test_kernel_times_and_launches_without_overlap(ada, ctx):
     """Every kernel of the calls is in the per-kernel timing; without dependent launches the results are the same."""
     c = Case(ada, 31, 8, 2, 64, 16, [70, 1], [900, 300])
