@@ -479,6 +479,11 @@ def _int32(t: torch.Tensor, name: str, n: Optional[int] = None, device: Optional
         raise ValueError(f"{name} must be dense with at least {n} entries")
 
 
+def _elsewhere(where: str) -> None:
+    """The tensors have been compared with the cache's device, and the cache with the context's."""
+    raise AdaError(1, f"{where}: the cache is not on the context's device")
+
+
 def _ragged(cache: KVCache, off: torch.Tensor, length: torch.Tensor) -> int:
     """Sequences of a call: off has one entry more than there are, the table and the lengths one for each."""
     B = off.numel() - 1
@@ -547,6 +552,8 @@ def ada_cache_append(ctx: Context, cache: KVCache, K: torch.Tensor, V: torch.Ten
         _int32(rep_idx, "rep_idx", N, cache.index)
     if rep_cnt is not None:
         _int32(rep_cnt, "rep_cnt", B, cache.index)
+    if cache.index != ctx.device or cache.index < 0:
+        _elsewhere("ada_cache_append")
     st = _fast.cache_append(ctx.addr, cache.addr, B, off, length, len_out, N, K, ldk, V, ldv, cache.dtype, Q, h, ldq, q_out,
                             ldqo, q_norm, k_norm, eps, inv_freq, 0 if inv_freq is None else 2 * inv_freq.numel(), pos0,
                             rep_idx, rep_cnt, flags, _stream_of(ctx, stream))
@@ -566,6 +573,8 @@ def ada_attention_cached(ctx: Context, cache: KVCache, Q: torch.Tensor, off: tor
     if out is None:
         out = _fresh(stream, Q.new_zeros, Q, (N, h, cache.d_h))
     _, _, ldo = _rows_of(out, "out", cache, N, h)
+    if cache.index != ctx.device or cache.index < 0:
+        _elsewhere("ada_attention_cached")
     st = _fast.attention_cached(ctx.addr, cache.addr, B, off, length, N, max_new, Q, h, ldq, cache.dtype, scale, out, ldo,
                                 flags, _stream_of(ctx, stream))
     if st:
@@ -596,6 +605,8 @@ def ada_select_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: torch.
         raise ValueError("blk_idx and blk_cnt are given together")
     else:
         _lists_of(cache, N, blk_idx, blk_cnt, k)
+    if cache.index != ctx.device or cache.index < 0:
+        _elsewhere("ada_select_blocks")
     st = _fast.select_blocks(ctx.addr, cache.addr, B, off, length, N, Q, h, ldq, cache.dtype, k, n_first, n_last, blk_idx,
                              blk_cnt, flags, _stream_of(ctx, stream))
     if st:
@@ -613,6 +624,8 @@ def ada_attention_blocks(ctx: Context, cache: KVCache, Q: torch.Tensor, off: tor
     if out is None:
         out = _fresh(stream, Q.new_zeros, Q, (N, h, cache.d_h))
     _, _, ldo = _rows_of(out, "out", cache, N, h)
+    if cache.index != ctx.device or cache.index < 0:
+        _elsewhere("ada_attention_blocks")
     st = _fast.attention_blocks(ctx.addr, cache.addr, B, off, length, N, Q, h, ldq, cache.dtype, blk_idx, blk_cnt, k, scale,
                                 out, ldo, flags, _stream_of(ctx, stream))
     if st:

@@ -209,6 +209,40 @@ def test_call_tensors(ada):
             call()
 
 
+@pytest.mark.parametrize("index,device", [(-1, 0), (1, 0), (0, 1), (-1, -1)])
+def test_a_cache_on_another_device_than_the_context(ada, monkeypatch, index, device):
+    """A cache in host memory, or on a GPU that is not the context's: nothing of it reaches the library."""
+    from types import SimpleNamespace
+
+    class There(torch.Tensor):
+        """A CPU tensor that says where it is."""
+        def get_device(self):
+            return index
+
+    reached = []
+    native = SimpleNamespace(**{name: lambda *a: reached.append(a) or 0 for name in
+                                ("cache_append", "attention_cached", "select_blocks", "attention_blocks")})
+    monkeypatch.setattr(ada, "_fast", native)
+    g = lambda t: t.as_subclass(There)                                                       # noqa: E731
+    stream = SimpleNamespace(cuda_stream=0)
+    c = ada.KVCache(g(bf(5, 2, 16, 64)), g(bf(5, 2, 16, 64)), g(torch.zeros((3, 4), dtype=torch.int32)), g(bf(5, 2, 64)),
+                    g(bf(5, 2, 64)))
+    Q, K, off, n = g(bf(7, 4, 64)), g(bf(7, 2, 64)), g(i32(0, 3, 7)), g(i32(5, 9))
+    idx, cnt = g(torch.zeros((7, 2, 4), dtype=torch.int32)), g(torch.zeros((7, 2), dtype=torch.int32))
+    calls = (lambda x: ada.ada_attention_cached(x, c, Q, off, n, 4, out=Q, stream=stream),
+             lambda x: ada.ada_select_blocks(x, c, Q, off, n, 4, blk_idx=idx, blk_cnt=cnt, stream=stream),
+             lambda x: ada.ada_attention_blocks(x, c, Q, off, n, idx, cnt, out=Q, stream=stream),
+             lambda x: ada.ada_cache_append(x, c, K, K, off, n, len_out=off[:2].clone(), stream=stream))
+    for call in calls:
+        with pytest.raises(ada.AdaError, match="device") as e:
+            call(SimpleNamespace(addr=4096, device=device))
+        assert e.value.status == 1 and not reached
+        if index >= 0:
+            call(SimpleNamespace(addr=4096, device=index))
+            assert len(reached) == 1
+            reached.clear()
+
+
 def test_outputs_are_made_on_the_stream_of_the_call(ada, monkeypatch):
     """What a call allocates or clears for itself is ordered with its kernels: made under the stream that was passed."""
     import contextlib
