@@ -450,6 +450,8 @@ class KVCache:
                 raise ValueError("a page of K or V must be dense: (h_kv, page_size, d_h)")
         if table.dim() != 2 or table.stride(1) != 1:
             raise ValueError("table must be (B, pages) with unit inner stride")
+        if table.shape[0] > 1 and table.stride(0) < table.shape[1]:
+            raise ValueError("the rows of table must not overlap")
         _int32(table, "table")
         if (kmin is None) != (kmax is None):
             raise ValueError("kmin and kmax belong together")
@@ -465,7 +467,7 @@ class KVCache:
         self.K_dtype, self.index = K.dtype, K.get_device()
         self.dtype, self.h_kv, self.d_h, self.page_size, self.B = dtype, h_kv, d, ps, table.shape[0]
         self._c = _KVCacheStruct(K.data_ptr(), V.data_ptr(), _ptr(kmin), _ptr(kmax), table.data_ptr(),
-                                 max(table.stride(0), table.shape[1]), table.shape[1], n,
+                                 table.stride(0) if table.shape[0] > 1 else table.shape[1], table.shape[1], n,
                                  K.stride(0) if n > 1 else h_kv * ps * d, ps, h_kv, d)
         self.addr = C.addressof(self._c)
 

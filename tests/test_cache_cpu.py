@@ -162,6 +162,22 @@ def test_cache_tensors(ada):
             ada.KVCache(*args)
 
 
+def test_tables_whose_rows_overlap(ada):
+    """Rows one behind the other in memory are read at the table's stride: one row expanded to several, or rows closer than
+    they are long, would be read where the table is not."""
+    K, V = bf(5, 2, 16, 64), bf(5, 2, 16, 64)
+    flat = torch.zeros(64, dtype=torch.int32)
+    for table in (flat[:4].view(1, 4).expand(3, 4), flat.as_strided((3, 4), (3, 1)), flat.as_strided((2, 4), (1, 1))):
+        with pytest.raises(ValueError, match="overlap"):
+            ada.KVCache(K, V, table)
+    for table, ld in ((flat.as_strided((3, 4), (4, 1)), 4), (flat.as_strided((3, 4), (9, 1)), 9), (flat[:4].view(1, 4), 4),
+                      (flat[:4].view(1, 4).expand(1, 4), 4), (flat.as_strided((1, 4), (2, 1)), 4), (flat.as_strided((1, 4), (50, 1)), 4)):
+        c = ada.KVCache(K, V, table)
+        assert c._c.table_ld == ld and c._c.max_pages == 4
+        last = (table.shape[0] - 1) * ld + 3               # what a kernel reads of it lies in it
+        assert last <= sum((n - 1) * s for n, s in zip(table.shape, table.stride()) if n > 1)
+
+
 def test_call_tensors(ada):
     from types import SimpleNamespace
     ctx = SimpleNamespace(addr=None, device=0)
