@@ -357,9 +357,10 @@ ada_status ada_cache_append(ada_ctx* ctx, const ada_kv_cache* cache, int64_t B, 
  *   flags    ADA_ATTN_CAUSAL: the sequence's new tokens are its last ones, and each sees the slots up to its own;
  *            0: each sees all len[b] slots
  *   scale    of the scores; 0: 1 / sqrt(d_h).  Not negative
- *   out      bf16, rows of h heads; may be Q itself (then ldo = ldq).  A token that sees no slot gets zeros; one that sees
- *            a NaN in a key, or whose scores leave the range of fp32, gets NaN.  A value that is NaN or infinite makes its
- *            element so for the tokens that see its slot; those that do not are not affected
+ *   out      bf16, rows of h heads; may be Q itself (then ldo = ldq).  A token that sees no slot gets zeros.  In fp32, with
+ *            the scale: a score of -inf has no weight; a token that has one of NaN or +inf, or sees slots but has none
+ *            but -inf, gets NaN.  A value that is NaN or infinite makes its element so for the tokens that see its slot;
+ *            those that do not are not affected
  * Scores, softmax statistics and sums in fp32; the probabilities are rounded to bf16 for the second product.
  * The first call on a context allocates its workspace (40 MB): make it before capturing into a CUDA graph.
  */

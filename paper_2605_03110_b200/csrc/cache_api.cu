@@ -1,4 +1,5 @@
 // C ABI of the paged key / value cache: argument checks, views, which kernel a call takes.
+#include <float.h>
 #include <math.h>
 
 #include "api_util.h"
@@ -42,9 +43,11 @@ cudaError_t ensure_cache_ws(ada_ctx* ctx, cudaStream_t s) {
     return cudaSuccess;
 }
 
-// scale of the scores, times log2(e)
+// scale of the scores, times log2(e).  Not 0 where fp32 has nothing smaller: 0 times a masked score, -inf, is NaN.
+// (2^-149 times the largest product of fp32 is 5e-7: equal weights either way.)
 float score_scale(double scale, int64_t d) {
-    return (float)((scale == 0.0 ? 1.0 / sqrt((double)d) : scale) * 1.4426950408889634);
+    const float f = (float)((scale == 0.0 ? 1.0 / sqrt((double)d) : scale) * 1.4426950408889634);
+    return f == 0.f ? FLT_TRUE_MIN : f;
 }
 
 }  // namespace

@@ -667,8 +667,10 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                 if (sh.odd_item == k) restore_values<NDB>(t_o, lim, sh);
             }
             __nv_bfloat16* dst = j.out + (int64_t)(it.row0 + tok_i) * j.ldo + ((int64_t)it.head * G + g) * c.d;
+            // of a row whose sum is 0: it sees no slot, and gets zeros, or all of its scores are -inf
+            const float none = lim > 0 ? NAN : 0.f;
             if (it.pieces == 1) {
-                const float f = l == 0.f ? 0.f : 1.0f / l;                   // (NaN stays)
+                const float f = l == 0.f ? none : 1.0f / l;                  // (NaN stays)
 #pragma unroll
                 for (int q = 0; q < NDB * 2; ++q) {
                     unsigned y[32];
@@ -737,7 +739,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                         L = fmaf(own ? l : __ldcg(part(p) + 128 * 256 + 256 + at),
                                  ex2_approx((own ? m : __ldcg(part(p) + 128 * 256 + at)) - Mr), L);
                     }
-                    const float f = L == 0.f ? 0.f : 1.0f / L;
+                    const float f = L == 0.f ? none : 1.0f / L;
                     // 64 columns at a time, in the order of the keys whoever joins them
 #pragma unroll 1
                     for (int q = 0; q < NDB; ++q) {

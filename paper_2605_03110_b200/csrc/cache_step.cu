@@ -451,7 +451,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                             const float mn = fmaxf(m[nt][i], x);
                             const float f = m[nt][i] > -INFINITY ? ex2_approx(m[nt][i] - mn) : 0.f;
                             m[nt][i] = mn;
-                            l[nt][i] *= f;
+                            l[nt][i] = top[nt][i] < INFINITY ? l[nt][i] * f : NAN;   // (a score beyond fp32: NaN, on every path)
 #pragma unroll
                             for (int d = 0; d < KS; ++d) { o[d][nt][i] *= f; o[d][nt][2 + i] *= f; }
                         }
@@ -559,10 +559,23 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
             const int t = LIST ? 0 : row / G, g = s.g0 + (LIST ? row : row - t * G);
             return j.out + (int64_t)(s.row + t) * j.ldo + ((int64_t)s.head * G + g) * c.d;
         };
+        // what a row whose sum is 0 gets: zeros if it sees no slot, NaN if all of its scores are -inf
+        auto no_weight = [&](int row) {
+            bool sees;
+            if (LIST) {                                // the first listed page has the first slot
+                const int p = s.cnt > 0 ? j.blk_idx[((int64_t)s.row * c.h_kv + s.head) * j.k] : c.max_pages;
+                sees = p < c.max_pages && (p << c.shift) < s.len;
+            } else {
+                sees = (j.causal ? s.len - s.n + row / G + 1 : s.len) > 0;
+            }
+            return sees ? NAN : 0.f;
+        };
         if (TEAM == 1) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float f[2] = {l[nt][0] == 0.f ? 0.f : 1.0f / l[nt][0], l[nt][1] == 0.f ? 0.f : 1.0f / l[nt][1]};   // (NaN stays)
+                float f[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) f[i] = l[nt][i] == 0.f ? no_weight(nt * 8 + c0 + i) : 1.0f / l[nt][i];   // (NaN stays)
                 __nv_bfloat16* dst = out_row(nt * 8 + r0);
 #pragma unroll
                 for (int d = 0; d < KS; ++d)
@@ -606,7 +619,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                     x = fmaf(mrg[(q * 8 + rr) * W + col], f, x);
                 }
                 if (s.pieces == 1) {
-                    if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L == 0.f ? 0.f : x / L);
+                    if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L == 0.f ? no_weight(row) : x / L);
                 } else {
                     mine[row * 128 + col] = x;
                     if (col == 0) { mine[2048 + row] = M; mine[2064 + row] = L; }
@@ -636,7 +649,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                         L = fmaf(__ldcg(part + 2064 + row), f, L);
                         x = fmaf(__ldcg(part + row * 128 + col), f, x);
                     }
-                    if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L == 0.f ? 0.f : x / L);
+                    if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L == 0.f ? no_weight(row) : x / L);
                 }
             }
             __syncthreads();

@@ -326,6 +326,62 @@ def test_nan_in_values_of_one_sequence(ada, ctx, news, lens, h, hk):
         assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num()), (b, j)
 
 
+SPANS = [([1], [900]), ([3], [900]), ([90], [900]), ([700], [900]), ([6], [4]), ([90], [80])]
+
+
+@pytest.mark.parametrize("how", ["causal", "lists"])
+@pytest.mark.parametrize("news,lens", SPANS)
+def test_scores_beyond_fp32(ada, ctx, news, lens, how):
+    """Scores that leave the range of fp32, in the product or only with the scale: NaN in every row that sees a slot, on
+    every path, where one is +inf or all are -inf; zeros where there is none."""
+    c = Case(ada, 27, 4, 2, 128, 32, news, lens)
+    n, length = news[0], lens[0]
+    some = torch.tensor([ref.sees(n, length, i, True) > 0 for i in range(n)])
+    scaled = lambda s: (attend_by(ada, ctx, c, how) if s is None else call(s)).cpu()          # noqa: E731
+
+    def call(scale):
+        if how != "lists":
+            return ada.ada_attention_cached(ctx, c.cache, c.d_Q, c.d_off, c.d_len, c.max_new, scale=scale)
+        pages = -(-length // 32)
+        idx = torch.arange(pages, dtype=torch.int32, device="cuda").expand(n, 2, pages).contiguous()
+        cnt = torch.full((n, 2), pages, dtype=torch.int32, device="cuda")
+        return ada.ada_attention_blocks(ctx, c.cache, c.d_Q, c.d_off, c.d_len, idx, cnt, scale=scale)
+
+    def nan_rows(out):
+        fine(ada, ctx)
+        assert bool((out[~some] == 0).all()) and bool(out[some].isnan().all())
+
+    c.cache.K.mul_(2.0 ** 40)                            # a product of 2^40, times 1e30
+    nan_rows(scaled(1e30))
+    Q = c.d_Q
+    c.cache.K.copy_(torch.where(c.cpu.K.isnan(), c.cpu.K, torch.full_like(c.cpu.K, 1e30)))
+    for sign in (1.0, -1.0):                             # the product itself; every score -inf
+        c.d_Q = torch.full_like(Q, sign * 1e30)
+        nan_rows(scaled(None))
+    # every score -inf but one slot's: that slot has all the weight
+    slot = max(length - n, 0)
+    page = int(c.cpu.table[0, slot // 32])
+    c.cache.K[page, :, slot % 32] = 0.0
+    out = scaled(None)
+    fine(ada, ctx)
+    v = c.cpu.V[page, :, slot % 32].repeat_interleave(2, 0)
+    assert bool((out[~some] == 0).all()) and torch.equal(out[some], v.expand(int(some.sum()), 4, 128))
+
+
+@pytest.mark.parametrize("scale", [1e-300, 1e-50, 1e-44, 1e-39, 1e-30])
+@pytest.mark.parametrize("news,lens", SPANS)
+def test_tiny_scale(ada, ctx, news, lens, scale):
+    """A scale that fp32 holds as a subnormal number, or not at all: equal weights, as far as a row sees."""
+    c = Case(ada, 28, 4, 2, 128, 32, news, lens)
+    pages = -(-lens[0] // 32)
+    idx = torch.arange(pages, dtype=torch.int32, device="cuda").expand(c.N, 2, pages).contiguous()
+    cnt = torch.full((c.N, 2), pages, dtype=torch.int32, device="cuda")
+    for out in (ada.ada_attention_cached(ctx, c.cache, c.d_Q, c.d_off, c.d_len, c.max_new, scale=scale),
+                ada.ada_attention_blocks(ctx, c.cache, c.d_Q, c.d_off, c.d_len, idx, cnt, scale=scale)):
+        fine(ada, ctx)
+        c.check(out, True, scale=scale)
+
+
 @pytest.mark.parametrize("news,lens", [([1] * 5, [3, 900, 64, 2000, 1]), ([200], [5000]), ([1, 90, 2, 300], [700, 90, 2, 1000])])
 def test_output_over_the_queries(ada, ctx, news, lens):
     c = Case(ada, 22, 8, 2, 128, 64, news, lens)
