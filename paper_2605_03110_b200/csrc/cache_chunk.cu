@@ -48,7 +48,7 @@ struct ChunkShared {
     long long range[3];                           // first place, one past the last, places per CTA
     struct { int slot, from, to, found[2]; } look; // values to look at: number of the slot's load (-1: no more), its rows; answers
     int odd_item;                                 // the CTA's latest item (from 1) with entries in here:
-    int odd[3][128];                              // first key whose value in a column is NaN, inf, -inf (see clean_values)
+    int odd[2][128];                              // first key whose value in a column is inf, -inf; NaN: both (see clean_values)
 };
 template <int NDB> __host__ __device__ constexpr int ch_smem() { return 14 * BLK_BYTES + (int)sizeof(ChunkShared); }
 static_assert(ch_smem<2>() <= 227 * 1024, "shared memory budget");
@@ -210,17 +210,12 @@ __device__ __forceinline__ void clean_values(unsigned char* v, int from, int to,
     for (int q = from * 8 + lane; q < to * 8; q += 32)
         for (int db = 0; db < NDB; ++db) {
             uint4* at = reinterpret_cast<uint4*>(v + db * BLK_BYTES + q * 16);
-            uint4 x = *at;
-            if (!nonfinite8(x)) continue;
-            unsigned* u = reinterpret_cast<unsigned*>(&x);
-            for (int e = 0; e < 8; ++e) {
-                const unsigned h = u[e >> 1] >> (16 * (e & 1)) & 0xffffu;
-                if ((h & 0x7f80u) != 0x7f80u) continue;
-                const int kind = (h & 0x7fu) != 0u ? 0 : h >> 15 ? 2 : 1;
-                atomicMin(&sh.odd[kind][db * 64 + (((q & 7) ^ ((q >> 3) & 7)) << 3) + e], key0 + (q >> 3));
-                u[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
-            }
-            *at = x;
+            if (!nonfinite8(*at)) continue;
+            const int key = q >> 3, col = db * 64 + (((q & 7) ^ (key & 7)) << 3);
+            take_nonfinite(at, [&](int e, bool pos, bool neg) {
+                if (pos) atomicMin(&sh.odd[0][col + e], key0 + key);
+                if (neg) atomicMin(&sh.odd[1][col + e], key0 + key);
+            });
         }
 }
 // the accumulator in TMEM of a row that sees `lim` keys
@@ -235,9 +230,8 @@ __device__ __forceinline__ void restore_values(unsigned t_o, int lim, const Chun
         for (int e = 0; e < 32; ++e) {
             const int col = q * 32 + e;
             float x = __uint_as_float(y[e]);
-            if (lim > sh.odd[0][col]) x = NAN;
-            if (lim > sh.odd[1][col]) x += INFINITY;
-            if (lim > sh.odd[2][col]) x -= INFINITY;
+            if (lim > sh.odd[0][col]) x += INFINITY;
+            if (lim > sh.odd[1][col]) x -= INFINITY;
             y[e] = __float_as_uint(x);
         }
         tmem_st32(t_o + q * 32, y);
@@ -495,7 +489,7 @@ k_cache_chunk(const __grid_constant__ ChunkMaps maps, const CacheView c, const R
                                 if (n_o[t] > 0) ok = ok && mbar_wait(&sh.o_empty[t], (n_o[t] - 1u) & 1u, abort_flag, 44);
                             ok = __all_sync(0xffffffffu, ok);
                             if (!ok) break;
-                            for (int q = lane; q < 3 * 128; q += 32) sh.odd[0][q] = INT_MAX;
+                            for (int q = lane; q < 2 * 128; q += 32) sh.odd[0][q] = INT_MAX;
                             __syncwarp();
                         }
                         clean_values<NDB>(ring + (sv % SLOTS) * SLOT_BYTES, sh.look.from, sh.look.to, (it.ku + u) * CH_KEYS, lane, sh);

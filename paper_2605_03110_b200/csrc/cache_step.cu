@@ -53,6 +53,8 @@ struct StepShared {
     float m[ST_WARPS][16], l[ST_WARPS][16];
     int abort_flag[2];
     int last;
+    int odd_any;                          // dense, of the row tile: a value of a later token was not finite
+    unsigned odd[128];                    // by column: bits 0..15 +inf, 16..31 -inf (NaN both) of token 0's successors 1..16
 };
 template <int NDB> __host__ __device__ constexpr int st_smem() {
     return st_ring_bytes<NDB>() + st_merge_bytes<NDB>() + (int)sizeof(StepShared);
@@ -182,12 +184,14 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
     if (tid == 0) {
         sh.abort_flag[0] = 0;
         sh.abort_flag[1] = wait_limit_units(false);
+        sh.odd_any = 0;
     }
     if (lane == 0) {
         for (int i = 0; i < SLOTS; ++i) mbar_init(&sh.full[warp][i], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
+    if (!LIST && tid < 128) sh.odd[tid] = 0u;
     if (tid == 64) { prefetch_map(&maps.k); prefetch_map(&maps.v); }
     __syncthreads();
     grid_dep_wait();
@@ -479,73 +483,37 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
             if (ok) {
                 const int st = used % SLOTS;
                 // Values that a row does not see must not meet its zero probability as a NaN or an infinity: those of slots that
-                // hold nothing of this sequence become zeros; if one of a later token is not finite, every token gets its products
-                // with zeros from its own limit on.
-                bool apart = false;
+                // hold nothing of this sequence become zeros, and so do a later token's that are not finite; rows that see one
+                // get it back where the warps' shares are joined.
                 if (base.x + 15 >= lim_all || base.y + 15 >= lim_all) {
                     unsigned char* v = ring + st * st_slot_bytes<NDB>();
-                    bool odd = false;
                     for (int q = lane; q < GK * NDB * 8; q += 32) {
                         const int key = (q >> 3) & 31, db = q >> 8;
                         const int pos = key < 16 ? base.x + key : base.y + key - 16;
                         uint4* at = reinterpret_cast<uint4*>(v + db * BLOCK + key * 128 + (q & 7) * 16);
-                        if (pos >= s.len) *at = make_uint4(0u, 0u, 0u, 0u);
-                        else if (!LIST && pos >= lim_all) odd = odd || nonfinite8(*at);
+                        if (pos >= s.len) {
+                            *at = make_uint4(0u, 0u, 0u, 0u);
+                        } else if (!LIST && pos >= lim_all && nonfinite8(*at)) {
+                            const int later = pos - lim_all, col = db * 64 + (((q & 7) ^ (key & 7)) << 3);   // token later + 1 on sees it
+                            sh.odd_any = 1;
+                            take_nonfinite(at, [&](int e, bool plus, bool minus) {
+                                if (later < 16) atomicOr(&sh.odd[col + e], ((plus ? 1u : 0u) | (minus ? 0x10000u : 0u)) << later);
+                            });
+                        }
                     }
-                    if (!LIST) apart = __any_sync(0xffffffffu, odd);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the slot's next load comes through the async proxy)
                     __syncwarp();
                 }
                 const unsigned vt = ring_u + st * st_slot_bytes<NDB>();
-                auto v_at = [&](int mt, int d) {
-                    return vt + (d >> 2) * BLOCK + (mt * 16 + v_key) * 128 + ((((d & 3) * 2 + v_ch) ^ (v_key & 7)) << 4);
-                };
-                if (!apart) {
 #pragma unroll
-                    for (int mt = 0; mt < 2; ++mt)
+                for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                        for (int d = 0; d < KS; ++d) {
-                            unsigned a[4];
-                            ldsm4t(v_at(mt, d), a);
+                    for (int d = 0; d < KS; ++d) {
+                        unsigned a[4];
+                        ldsm4t(vt + (d >> 2) * BLOCK + (mt * 16 + v_key) * 128 + ((((d & 3) * 2 + v_ch) ^ (v_key & 7)) << 4), a);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma16816(o[d][nt], a, pf[mt][nt][0], pf[mt][nt][1]);
-                        }
-                } else {
-                    // from the last token, which sees the most, to the first; of each product the token's own rows are kept
-#pragma unroll 1
-                    for (int t = (s.rows + G - 1) / G - 1; t >= 0; --t) {
-                        unsigned char* v = ring + st * st_slot_bytes<NDB>();
-                        for (int q = lane; q < GK * NDB * 8; q += 32) {
-                            const int key = (q >> 3) & 31, db = q >> 8;
-                            if ((key < 16 ? base.x + key : base.y + key - 16) >= lim_all + t)
-                                *reinterpret_cast<uint4*>(v + db * BLOCK + key * 128 + (q & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                        }
-                        __syncwarp();
-#pragma unroll
-                        for (int d = 0; d < KS; ++d) {
-                            float x[NT][4];
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) x[nt][e] = o[d][nt][e];
-#pragma unroll
-                            for (int mt = 0; mt < 2; ++mt) {
-                                unsigned a[4];
-                                ldsm4t(v_at(mt, d), a);
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) mma16816(x[nt], a, pf[mt][nt][0], pf[mt][nt][1]);
-                            }
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if ((nt * 8 + c0 + (e & 1)) / G == t) o[d][nt][e] = x[nt][e];
-                        }
-                        __syncwarp();                 // all lanes have read the values
+                        for (int nt = 0; nt < NT; ++nt) mma16816(o[d][nt], a, pf[mt][nt][0], pf[mt][nt][1]);
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                }
             }
             release();
         }
@@ -592,6 +560,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
         constexpr int W = NDB * 64;
         const int col = tid % W;
         float* mine = partial<LIST>(ws, s, s.piece);
+        int odd = 0;
         if (lane < 4)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -606,6 +575,7 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                 for (int e = 0; e < 4; ++e)
                     mrg[(warp * 8 + c0 + (e & 1)) * W + d * 16 + (e >> 1) * 8 + r0] = o[d][nt][e];
             __syncthreads();
+            if (!LIST && nt == 0) odd = sh.odd_any;
             const int rows = min(s.rows - nt * 8, 8);
             for (int rr = tid / W; rr < rows; rr += THREADS / W) {
                 const int row = nt * 8 + rr;
@@ -618,6 +588,11 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                     L = fmaf(sh.l[q][row], f, L);
                     x = fmaf(mrg[(q * 8 + rr) * W + col], f, x);
                 }
+                if (!LIST && odd) {                    // what the row's token sees of the values that were taken out
+                    const unsigned seen = sh.odd[col] & ((1u << row / G) - 1u) * 0x10001u;
+                    if (seen & 0xffffu) x += INFINITY;
+                    if (seen >> 16) x -= INFINITY;
+                }
                 if (s.pieces == 1) {
                     if (col < c.d) out_row(row)[col] = __float2bfloat16_rn(L == 0.f ? no_weight(row) : x / L);
                 } else {
@@ -626,6 +601,11 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                 }
             }
             __syncthreads();                           // the buffer is reused
+        }
+        if (!LIST && odd) {                            // (the same in all threads)
+            if (tid < 128) sh.odd[tid] = 0u;
+            if (tid == 0) sh.odd_any = 0;
+            __syncthreads();
         }
         if (s.pieces > 1) {
             __threadfence();

@@ -95,6 +95,21 @@ static __device__ __forceinline__ bool nonfinite8(const uint4& w) {
     return (y & 0x7fff7fffu) != 0u;
 }
 
+// Takes the elements that are not finite out of eight bf16 in shared memory: put(element, as +inf, as -inf), a NaN as both
+// (what is added to a sum in their stead later: +inf and -inf make NaN).
+template <typename F>
+static __device__ __forceinline__ void take_nonfinite(uint4* at, F put) {
+    unsigned* u = reinterpret_cast<unsigned*>(at);
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) {
+        const unsigned h = u[e >> 1] >> (16 * (e & 1)) & 0xffffu;
+        if ((h & 0x7f80u) != 0x7f80u) continue;
+        const bool nan = (h & 0x7fu) != 0u;
+        put(e, nan || h == 0x7f80u, nan || h != 0x7f80u);
+        u[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
+    }
+}
+
 // transposes an 8 x 8 matrix of 16-bit elements held as a matrix fragment (two elements of a row per lane)
 static __device__ __forceinline__ unsigned transposed(unsigned x) {
     unsigned y;
