@@ -487,16 +487,23 @@ k_cache_step(const __grid_constant__ StepMaps maps, const CacheView c, const Rag
                 // get it back where the warps' shares are joined.
                 if (base.x + 15 >= lim_all || base.y + 15 >= lim_all) {
                     unsigned char* v = ring + st * st_slot_bytes<NDB>();
-                    for (int q = lane; q < GK * NDB * 8; q += 32) {
-                        const int key = (q >> 3) & 31, db = q >> 8;
-                        const int pos = key < 16 ? base.x + key : base.y + key - 16;
-                        uint4* at = reinterpret_cast<uint4*>(v + db * BLOCK + key * 128 + (q & 7) * 16);
-                        if (pos >= s.len) {
-                            *at = make_uint4(0u, 0u, 0u, 0u);
-                        } else if (!LIST && pos >= lim_all && nonfinite8(*at)) {
-                            const int later = pos - lim_all, col = db * 64 + (((q & 7) ^ (key & 7)) << 3);   // token later + 1 on sees it
+                    auto position = [&](int q) {           // of 16-byte piece q of a granule
+                        const int key = (q >> 3) & 31;
+                        return key < 16 ? base.x + key : base.y + key - 16;
+                    };
+                    auto piece = [&](int q) {
+                        return reinterpret_cast<uint4*>(v + (q >> 8) * BLOCK + ((q >> 3) & 31) * 128 + (q & 7) * 16);
+                    };
+                    for (int q = lane; q < GK * NDB * 8; q += 32)
+                        if (position(q) >= s.len) *piece(q) = make_uint4(0u, 0u, 0u, 0u);
+                    if (!LIST && lim_all < s.len) {
+#pragma unroll 1
+                        for (int q = lane; q < GK * NDB * 8; q += 32) {
+                            const int later = position(q) - lim_all;         // token later + 1 on sees it
+                            if (later < 0 || later >= s.len - lim_all || !nonfinite8(*piece(q))) continue;
+                            const int col = (q >> 8) * 64 + (((q & 7) ^ (q >> 3 & 7)) << 3);
                             sh.odd_any = 1;
-                            take_nonfinite(at, [&](int e, bool plus, bool minus) {
+                            take_nonfinite(piece(q), [&](int e, bool plus, bool minus) {
                                 if (later < 16) atomicOr(&sh.odd[col + e], ((plus ? 1u : 0u) | (minus ? 0x10000u : 0u)) << later);
                             });
                         }
