@@ -51,14 +51,15 @@ struct Lane {
     bool on, turns;                      // has elements; they are rotated
 };
 
-// cosines and sines of the lane's four pairs at position `pos`
-__device__ __forceinline__ void angles(const AppendJob& j, const Lane& ln, int v, int pos, float (&cs)[4], float (&sn)[4]) {
+// cosines and sines of the lane's four pairs at position p0 + i (which may be behind the largest int32)
+__device__ __forceinline__ void angles(const AppendJob& j, const Lane& ln, int v, int p0, int i, float (&cs)[4], float (&sn)[4]) {
+    const double pos = (double)p0 + (double)i;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        cs[i] = 1.f; sn[i] = 0.f;
+    for (int q = 0; q < 4; ++q) {
+        cs[q] = 1.f; sn[q] = 0.f;
         if (ln.turns) {
-            const double turns = (double)pos * j.inv_freq[4 * v + i] * 0.15915494309189533577;   // 1 / (2 pi)
-            sincospif(2.0f * (float)(turns - rint(turns)), &sn[i], &cs[i]);
+            const double turns = pos * j.inv_freq[4 * v + q] * 0.15915494309189533577;   // 1 / (2 pi)
+            sincospif(2.0f * (float)(turns - rint(turns)), &sn[q], &cs[q]);
         }
     }
 }
@@ -198,7 +199,7 @@ k_cache_append(const CacheView c, const Ragged r, const AppendJob j, int shares,
     ln.e0 = !PAIRS && ln.turns ? 4 * v : 8 * v;
     ln.e1 = !PAIRS && ln.turns ? 4 * v + (j.rot >> 1) : 8 * v + 4;
     float cs[4], sn[4];
-    angles(j, ln, v, p0 + li, cs, sn);
+    angles(j, ln, v, p0, li, cs, sn);
     bool bad = false;
     if (j.Q != nullptr && (!STEP || share < shares))
         move_rows<LG, PAIRS>(j.Q + (int64_t)i * j.ldq, j.q_out + (int64_t)i * j.ldqo, c.d, first, step, j.h, c.d, ln, j.q_norm,
@@ -220,7 +221,7 @@ k_cache_append(const CacheView c, const Ragged r, const AppendJob j, int shares,
             int turned = li;                                     // whose angles the lane has
             for (int t = last ? li - (slot - s0) : li; t <= li; ++t) {      // this token, or all new ones of the page
                 const int tok = j.rep_idx != nullptr ? min(max(j.rep_idx[o + t], 0), n - 1) : t;
-                if (tok != turned) angles(j, ln, v, p0 + tok, cs, sn);
+                if (tok != turned) angles(j, ln, v, p0, tok, cs, sn);
                 turned = tok;
                 uint2 a = make_uint2(0u, 0u), b2 = a;
                 if (ln.on) {
@@ -274,7 +275,7 @@ k_cache_append(const CacheView c, const Ragged r, const AppendJob j, int shares,
         }
     } else if (page >= 0) {
         const int64_t at0 = slot_at(c, page, 0, slot), head_step = (int64_t)c.d << c.shift;
-        if (at != li) angles(j, ln, v, p0 + at, cs, sn);
+        if (at != li) angles(j, ln, v, p0, at, cs, sn);
         move_rows<LG, PAIRS>(j.K + (int64_t)(o + at) * j.ldk, c.k + at0, head_step, first, step, c.h_kv, c.d, ln, j.k_norm, j.eps,
                              rotate, cs, sn, mask, bad);
         move_rows<LG, PAIRS>(j.V + (int64_t)(o + at) * j.ldv, c.v + at0, head_step, first, step, c.h_kv, c.d, ln, nullptr, 0.f,

@@ -648,6 +648,23 @@ def test_append_in_place_and_far_positions(ada, ctx):
     assert near(c.cache.K.cpu().nan_to_num(), want[0].nan_to_num(), 8.0)
 
 
+@pytest.mark.parametrize("news", [[5], [5, 0, 0, 0, 0, 1]])
+def test_positions_behind_the_largest_int32(ada, ctx, news):
+    """Positions go on behind 2^31 - 1, in both forms of the append (several tokens; no more rows than sequences)."""
+    B = len(news)
+    c = Case(ada, 46, 2, 2, 64, 32, news, [max(n, 1) for n in news])
+    f = 10000.0 ** (-torch.arange(0, 64, 2, dtype=torch.float64) / 64)
+    pos0 = [2 ** 31 - 3] * B
+    K, V = torch.randn(c.N, 2, 64).bfloat16(), torch.randn(c.N, 2, 64).bfloat16()
+    want = ref.append(c.cpu, K, V, c.off, [0] * B, c.Q, None, None, 1e-6, f, False, pos0)
+    q, _ = ada.ada_cache_append(ctx, c.cache, K.cuda(), V.cuda(), c.d_off, i32([0] * B), Q=c.d_Q, inv_freq=f.cuda(), pos0=i32(pos0))
+    fine(ada, ctx)
+    # (the angle, up to 2^31 radians, is rounded to 64 bits: 2^-22, times an element of up to 8, half of near()'s 2^-19 x 8)
+    assert near(q, want[4], 8.0)
+    for got, w in ((c.cache.K, want[0]), (c.cache.kmin, want[2]), (c.cache.kmax, want[3])):
+        assert near(got.cpu().nan_to_num(), w.nan_to_num(), 8.0)
+
+
 def test_append_of_representatives(ada, ctx):
     """Only the listed tokens are kept, rotated where they stood; the queries are not affected."""
     news, olds = [50, 20, 10], [3, 0, 8]
