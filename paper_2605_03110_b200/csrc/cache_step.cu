@@ -94,8 +94,18 @@ struct Work {                              // where a team is in its run of work
         if (LIST) {
             while (at < end) {
                 if (b < 0 || row < off || row >= off + n) {     // another sequence
+                    // Rows from off[B] on are nobody's.  One before that may be too if the offsets are out of order: all teams
+                    // that meet it leave it out, and each goes on, so that a row's pieces are all there or none of them
+                    // (what comes back to zero are the counters of the next call).
+                    const int last = r.off[r.B];
                     b = seq_of_row(r, row);
-                    if (b < 0) { at = end; return false; }      // (rows of no sequence come last)
+                    if (row >= last) { at = end; return false; }
+                    if (b < 0) {
+                        at += ((int64_t)(c.h_kv - head) * tiles - rt) * pieces - piece;
+                        head = rt = piece = 0;
+                        ++row;
+                        continue;
+                    }
                     load_seq(r, c, j.few);
                 }
                 s.b = b; s.head = head; s.row = row; s.g0 = rt * 16;

@@ -765,6 +765,34 @@ def test_bad_pages_and_offsets_are_reported(ada, ctx, max_new):
     assert torch.equal(out, good)
 
 
+@pytest.mark.parametrize("off", [[0, 3, 2, 3, 4], [0, 1, -5, 3, 4], [1, 2, 3, 4, 4], [3, 4, 0, 1, 2], [0, 1, 2, 1000, 4], [0, 0, 4, 4, 1]])
+def test_calls_after_faulty_offsets(ada, ctx, off):
+    """Whatever the offsets say, a call leaves the workspace as the next one needs it: nobody has asked for the status
+    (which would clear it) in between."""
+    c = Case(ada, 63, 8, 2, 64, 128, [1] * 4, [9000, 5000, 8192, 7000])
+    many = Case(ada, 64, 8, 2, 64, 64, [30, 40, 20, 50], [3000, 900, 700, 4000])
+    k = 64
+    idx = torch.arange(k, dtype=torch.int32, device="cuda").expand(4, 2, k).contiguous()
+    cnt = torch.full((4, 2), k, dtype=torch.int32, device="cuda")
+    cnt[1:] = torch.tensor([[40, 3], [64, 64], [55, 50]])
+
+    def run(o, o_many):
+        return (ada.ada_attention_blocks(ctx, c.cache, c.d_Q, o, c.d_len, idx, cnt),            # lists in pieces
+                ada.ada_attention_cached(ctx, c.cache, c.d_Q, o, c.d_len, 1),
+                ada.ada_attention_cached(ctx, many.cache, many.d_Q, o_many, many.d_len, 50))
+
+    good = run(c.d_off, many.d_off)
+    fine(ada, ctx)
+    bad = [run(i32(off), i32([30 * x for x in off])) for _ in range(3)]
+    after = [run(c.d_off, many.d_off) for _ in range(3)]
+    assert status(ada, ctx) == 5
+    assert all(torch.equal(x, y) for got in after for x, y in zip(got, good))
+    assert all(torch.equal(x, y) for got in bad for x, y in zip(got, bad[0]))
+    again = run(c.d_off, many.d_off)
+    fine(ada, ctx)
+    assert all(torch.equal(x, y) for x, y in zip(again, good))
+
+
 def test_bad_lists_are_reported(ada, ctx):
     c = Case(ada, 61, 4, 2, 64, 16, [1], [200])
     for idx, cnt in (([3, 3, 4], 3), ([4, 3, 5], 3), ([-1, 3, 4], 3), ([1, 2, 1000], 3), ([1, 2, 3], 4), ([1, 2, 3], -1)):
