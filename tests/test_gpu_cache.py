@@ -496,6 +496,49 @@ def test_select_near_ties(ada, ctx):
     assert lists_of(idx, cnt) == ref.select(c.cpu, c.Q, c.off, c.lens, 2, 40, 1, 1)
 
 
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("close", [2, 9, 30])
+@pytest.mark.parametrize("news,pages", [([1], 100), ([1], 700), ([1], 1500), ([3], 100), ([3], 700), ([5], 100), ([5], 700), ([16], 300)])
+def test_select_scores_that_fp32_cannot_tell_apart(ada, ctx, news, pages, close, sign):
+    """`close` pages around the last place differ by less than an fp32 score can show, all others by far more: few enough
+    to be scored again one by one, whose order in 64 bits runs against that of the pages."""
+    hk, d, ps = 2, 64, 16
+    n = news[0]
+    g = torch.Generator().manual_seed(pages + close)
+    table = torch.randperm(pages, generator=g).int().view(1, -1)
+    for above in (3, 40):                                    # places that are given for certain: few and many
+        bound = torch.zeros((pages, hk, d))
+        order = torch.randperm(pages, generator=g)
+        ahead, near_, rest = order[:above], order[above:above + close].sort().values, order[above + close:]
+        bound[ahead, :, 0] = 112.0
+        bound[rest, :, 0] = (8.0 + 0.25 * (torch.arange(len(rest)) % 128)).view(-1, 1)
+        bound[near_, :, 0] = 96.0
+        # 2^-14 (1 + i / 128), more for the higher page: 2^-21 a step, where a score of 96 has a last place of 2^-17
+        bound[near_, :, 1] = (1.0 + torch.arange(close) / 128.0).view(-1, 1)
+        bound[..., 0] *= sign
+        Q = torch.zeros((n, 4, d))
+        Q[..., 0] = sign
+        Q[..., 1] = 2.0 ** -14
+        Q *= 2.0 ** (torch.arange(n) % 3).view(-1, 1, 1)
+        Q = Q.bfloat16()
+        k_ = bound.bfloat16()
+        assert torch.equal(k_.float(), bound)
+        kmin = torch.empty_like(k_)
+        kmin[table[0].long()] = k_
+        KV = torch.zeros((pages, hk, ps, d), dtype=torch.bfloat16, device="cuda")
+        cache = ada.KVCache(KV, KV, table.cuda(), kmin.cuda(), kmin.cuda())
+        cpu = ref.Pages(KV, KV, table, kmin, kmin)
+        length = pages * ps
+        for need in {1, close // 2, close - 1} - {0}:
+            k = above + need
+            # causal tokens of one sequence: all of them see the last page
+            idx, cnt = ada.ada_select_blocks(ctx, cache, Q.cuda(), i32([0, n]), i32([length]), k, 0, 0)
+            fine(ada, ctx)
+            want = ref.select(cpu, Q, [0, n], [length], hk, k, 0, 0)
+            assert all(x == sorted(ahead.tolist() + near_[close - need:].tolist()) for row in want for x in row)
+            assert lists_of(idx, cnt) == want, (above, need)
+
+
 def test_select_infinite_bounds(ada, ctx):
     """A page whose score is NaN comes last, an infinite one first."""
     c = Case(ada, 23, 2, 2, 64, 16, [1], [1600])
