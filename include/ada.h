@@ -362,7 +362,8 @@ ada_status ada_cache_append(ada_ctx* ctx, const ada_kv_cache* cache, int64_t B, 
  *            but -inf, gets NaN.  A value that is NaN or infinite makes its element so for the tokens that see its slot;
  *            those that do not are not affected
  * Scores, softmax statistics and sums in fp32; the probabilities are rounded to bf16 for the second product.
- * The first call on a context allocates its workspace (40 MB): make it before capturing into a CUDA graph.
+ * The first call on a context allocates its workspace (40 MB): make it before capturing into a CUDA graph (while one is
+ * captured it is ADA_ERR_CUDA, and the capture goes on).
  */
 ada_status ada_attention_cached(ada_ctx* ctx, const ada_kv_cache* cache, int64_t B, const int32_t* off,
                                 const int32_t* len, int64_t N, int64_t max_new, const void* Q, int64_t h, int64_t ldq,

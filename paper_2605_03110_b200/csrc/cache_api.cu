@@ -30,10 +30,14 @@ ada_status open_cache(const ada_ctx* ctx, const ada_kv_cache* kv, int64_t B, con
 // graph keeps a valid pointer whatever is called later.
 cudaError_t ensure_cache_ws(ada_ctx* ctx, cudaStream_t s) {
     if (ctx->cache_ws != nullptr) return cudaSuccess;
+    // While a graph is captured the counters would be cleared by the graph's first replay, not now.
+    cudaStreamCaptureStatus capture;
+    cudaError_t e = cudaStreamIsCapturing(s, &capture);
+    if (e != cudaSuccess) return e;
+    if (capture != cudaStreamCaptureStatusNone) return cudaErrorStreamCaptureUnsupported;
     const size_t part = 2 * (size_t)ctx->sm_count * cache_part_floats() * 4, ctr = 8 * (size_t)ctx->sm_count * 4;
     char* p = nullptr;
-    cudaError_t e = cudaMalloc(&p, part + ctr);
-    if (e != cudaSuccess) return e;
+    if ((e = cudaMalloc(&p, part + ctr)) != cudaSuccess) return e;
     e = cudaMemsetAsync(p + part, 0, ctr, s);
     if (e != cudaSuccess) { cudaFree(p); return e; }
     ctx->cache_ws = p;

@@ -274,7 +274,7 @@ def attend_by(ada, ctx, c, how):
 @pytest.mark.parametrize("how", ["causal", "all", "lists"])
 @pytest.mark.parametrize("h,hk,d,ps,n,length", [(4, 2, 128, 32, 1, 900), (4, 2, 128, 32, 3, 900), (2, 2, 128, 64, 16, 500),
                                                 (3, 1, 48, 16, 4, 129), (4, 2, 128, 32, 90, 900), (4, 2, 128, 32, 700, 900),
-                                                (16, 1, 64, 128, 130, 130), (6, 1, 80, 16, 60, 40)])
+                                                (16, 1, 64, 128, 130, 130), (6, 1, 80, 16, 60, 40), (4, 2, 64, 16, 7, 5)])
 def test_nan_and_infinity_in_values(ada, ctx, h, hk, d, ps, n, length, how):
     """A value that is NaN or infinite makes its element so in the rows that see its slot, and changes nothing else: not a
     bit of the rows before it, whose probability of that slot is zero."""
@@ -973,6 +973,34 @@ def test_captured_step(ada, ctx):
         tol = ref.tolerance(want, weight, cpu.V.float().nan_to_num())
         assert bool(((out.cpu().double() - want).abs() <= tol).all())
     assert lists_of(idx, cnt) == ref.select(cpu, Q, c.off, [210, 70], hk, k, 1, 1)
+
+
+@pytest.mark.parametrize("mode", ["global", "relaxed"])
+def test_first_call_while_a_graph_is_captured(ada, mode):
+    """It would have to allocate: refused, the capture goes on, and the context serves as if nothing had been."""
+    own = ada.ada_create(1, 128, 128, ada.ADA_BF16)
+    c = Case(ada, 81, 8, 2, 64, 16, [1, 1], [3000, 70])
+    other = Case(ada, 82, 8, 2, 64, 16, [200], [300])
+    x = torch.zeros(4, device="cuda")
+    idx, cnt = torch.zeros((2, 2, 4), dtype=torch.int32, device="cuda"), torch.zeros((2, 2), dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, capture_error_mode=mode):
+        for call in (lambda: ada.ada_attention_cached(own, c.cache, c.d_Q, c.d_off, c.d_len, 1),
+                     lambda: ada.ada_attention_cached(own, other.cache, other.d_Q, other.d_off, other.d_len, 200),
+                     lambda: ada.ada_attention_blocks(own, c.cache, c.d_Q, c.d_off, c.d_len, idx, cnt)):
+            with pytest.raises(ada.AdaError) as e:
+                call()
+            assert e.value.status == 4
+        x += 1
+    for _ in range(3):
+        for y in (c, other):
+            y.check(ada.ada_attention_cached(own, y.cache, y.d_Q, y.d_off, y.d_len, y.max_new), True)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert x.tolist() == [1.0] * 4
+    fine(ada, own)
+    ada.ada_destroy(own)
 
 
 def test_prompt_to_generation(ada, ctx):
