@@ -438,7 +438,8 @@ def ada_attention_reps(ctx: Context, Q: torch.Tensor, K: torch.Tensor, V: torch.
 class KVCache:
     """Paged key / value cache: K and V (n_pages, h_kv, page_size, d_h) bf16, planes of one tensor or tensors of their
     own with the same page stride; table (B, pages of a sequence) int32; kmin, kmax (n_pages, h_kv, d_h) bf16, the
-    bounds of every page's keys (both or neither; ada_select_blocks needs them).  The tensors are the caller's."""
+    bounds of every page's keys (both or neither; ada_select_blocks needs them).  The tensors are the caller's.  Of a
+    table that is much wider than the longest sequence, table[:, :pages] makes ada_select_blocks faster."""
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, kmin: Optional[torch.Tensor] = None,
                  kmax: Optional[torch.Tensor] = None):

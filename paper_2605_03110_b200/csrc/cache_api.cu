@@ -105,7 +105,10 @@ ada_status ada_attention_cached(ada_ctx* ctx, const ada_kv_cache* cache, int64_t
     DeviceGuard guard(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     CU(ensure_cache_ws(ctx, s));
-    // rows of a key head that one 16-row tile of mma.sync holds, or tiles of 128 rows; several sequences may be mixed
+    // Up to as many rows of a key head as one 16-row tile of mma.sync holds, or tiles of 128 rows; several sequences may be
+    // mixed.  Both kernels, 32 heads on 8, us with 4, 8 and 16 rows, d_h 128: 16 sequences of 8192 91, 95, 104 (tiles of 128
+    // rows: 114, 118, 120), one of 8192 15, 21, 32 (32 each), one of 131072 96, 102, 119 (135 to 141); d_h 64: 51, 52, 58 (98), 11,
+    // 14, 20 (26), 55, 59, 69 (110).  17 to 128 rows take what 16 take there: 123 to 131, 32 to 34, 135 to 140; 107, 26, 111.
     const int few = 16 / (j.h / c.h_kv);
     if (j.max_new <= few) {
         CU(launch_cache_step(ctx, c, r, j, s));

@@ -8,7 +8,7 @@
 //   warps 2, 3  look at the values that not every row sees (a chunk's own): a NaN there must not reach the rows before it
 //   warps 4..7  softmax of tile 0, one row per thread: S out of TMEM into registers, 2^(s - m), P back into TMEM as bf16
 //               over its own scores, where the second product takes it from as its left operand
-//   warps 8..11 the same for tile 1 (they have most of the registers: a row's 128 scores stay in them)
+//   warps 8..11 the same for tile 1 (they have most of the registers, for a row's 128 scores)
 // V needs no transposed copy: its tiles are MN-major right operands as the pages hold them.
 // A row's reference maximum m is raised only when the running maximum has left it by more than 8 powers of two
 // (then the accumulator is rescaled in TMEM); O / l does not depend on it.
@@ -17,13 +17,17 @@
 // equal run of units.  An item that several CTAs share is joined, 32 rows at a time, by the warp that finishes last,
 // in the order of the keys; nobody waits for another CTA.
 //
-// Measured (32 heads on 8 key heads of 128): 2048 tokens after 6145 others 224 us = 1075 TFLOP/s, 65 % of cuBLAS's best.  Two
-// tiles and 128 keys take 3500 cycles, of them 2048 the tensor core's: each tile's chain is 600 for scores into registers
+// Measured (32 heads on 8 key heads of 128): 2048 tokens after 6145 others, called again and again, 264 us = 911 TFLOP/s, 65 %
+// of what cuBLAS sustains; a few calls on a GPU that was idle before (higher clocks) 228 us = 1055 TFLOP/s, 63 % of its
+// best.  Two tiles and 128 keys take 3500 cycles, of them 2048 the tensor core's: each tile's chain is 600 for scores into registers
 // and maxima, 1600 for exponentials (special-function unit and multipliers shared by the two sets), 1250 until the next
 // scores are there (half of the second product, the first one, the signals).  An item's output takes 2.8 us, a share's
-// 3.5, joining two shares 6 (11 before the last one's own came straight out of TMEM: 230 us).
-// On the way: MMAs issued behind `if (lane == 0)` 335 us, behind elect_one() 242; exponentials in two unrolled copies that
-// miss the instruction cache 253, in one 232.
+// 3.5, joining two shares 6 (11 before the last one's own came straight out of TMEM: 230 us against 224 at the time).
+// On the way, idle GPU: MMAs issued behind `if (lane == 0)` 335 us, behind elect_one() 242; exponentials in two unrolled copies
+// that miss the instruction cache 253, in one 232.
+// Registers: 352 bytes of spill stores and 400 of loads (d_h above 64; 344 and 380 up to it).  Compiled with the other roles
+// empty, the softmax role has 180 and 164 of them, nearly all with its key loop alone: 128 scores and 32 probabilities do
+// not leave room in 216 registers for all of an item's state.  The rest is the producer's and the issuer's, in 72.
 #include "cache_tma.cuh"
 
 namespace ada {

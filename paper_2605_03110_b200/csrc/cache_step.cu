@@ -18,9 +18,9 @@
 // whatever the lengths are, and a row tile that several CTAs share is joined by the one that finishes last (in
 // the order of the keys, so that results do not depend on who that is).  Nobody waits for another CTA.
 //
-// Measured (32 heads on 8 key heads of 128, pages of 64): 64 sequences of up to 16384 tokens, 2.2 GB, 338 us = 6.6 TB/s; two of
-// 131072 tokens 171 us = 6.3 TB/s; lists of 32 pages for 32 tokens 47 us = 5.7 TB/s (two row tiles for most CTAs, one for the
-// rest); lists of 16 pages for 1000 tokens 244 us, 4.2 GB out of L2.  With S = Q K^T and 16 rows padded, four warps:
+// Measured (32 heads on 8 key heads of 128, pages of 64): 64 sequences of up to 16384 tokens, 2.2 GB, 341 us = 6.5 TB/s; two of
+// 131072 tokens 170 us = 6.3 TB/s; lists of 32 pages for 32 tokens 48 us = 5.7 TB/s (two row tiles for most CTAs, one for the
+// rest); lists of 16 pages for 1000 tokens 247 us, 4.2 GB out of L2.  With S = Q K^T and 16 rows padded, four warps:
 // 355, 182, 51 and 480 us.
 #include "cache_tma.cuh"
 

@@ -496,6 +496,25 @@ def test_select_near_ties(ada, ctx):
     assert lists_of(idx, cnt) == ref.select(c.cpu, c.Q, c.off, c.lens, 2, 40, 1, 1)
 
 
+@pytest.mark.parametrize("width", [300, 1024, 2100, 4096, 8192, 16384])
+@pytest.mark.parametrize("news,lens", [([40, 1, 0, 3], [1500, 700, 20, 90]), ([1, 1, 1], [4000, 16, 333])])
+def test_wide_tables(ada, ctx, news, lens, width):
+    """A table for far longer texts than there are: the same pages, whether a call may look at all of it or at its front."""
+    c = Case(ada, 29, 4, 2, 64, 16, news, lens, pad=1, drift=0.5)
+    B, used = c.cache.table.shape
+    wide = torch.full((B, width), -3, dtype=torch.int32, device="cuda")
+    wide[:, :used] = c.cache.table
+    want = ref.select(c.cpu, c.Q, c.off, c.lens, 2, 9, 1, 1)[:c.off[-1]]
+    out = ada.ada_attention_cached(ctx, c.cache, c.d_Q, c.d_off, c.d_len, c.max_new)
+    for table in (wide, wide[:, :used], wide[:, :used + 100]):
+        cache = ada.KVCache(c.cache.K, c.cache.V, table, c.cache.kmin, c.cache.kmax)
+        idx, cnt = ada.ada_select_blocks(ctx, cache, c.d_Q, c.d_off, c.d_len, 9)
+        got = ada.ada_attention_cached(ctx, cache, c.d_Q, c.d_off, c.d_len, c.max_new)
+        fine(ada, ctx)
+        assert lists_of(idx[:c.off[-1]], cnt[:c.off[-1]]) == want
+        assert torch.equal(got, out)
+
+
 @pytest.mark.parametrize("sign", [1.0, -1.0])
 @pytest.mark.parametrize("close", [2, 9, 30])
 @pytest.mark.parametrize("news,pages", [([1], 100), ([1], 700), ([1], 1500), ([3], 100), ([3], 700), ([5], 100), ([5], 700), ([16], 300)])
